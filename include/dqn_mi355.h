@@ -39,6 +39,9 @@ enum { DQN_OK = 0, DQN_EINVAL = -1, DQN_EHIP = -2, DQN_ENOMEM = -3, DQN_ESTATE =
 
 enum { DQN_PRECISION_FP32 = 0, DQN_PRECISION_BF16 = 1 };
 
+/* element types of the matrices that the calls without a handle take */
+enum { DQN_TYPE_FP32 = 0, DQN_TYPE_BF16 = 1, DQN_TYPE_FP16 = 2 };
+
 /* dqn_get_params / dqn_set_params selector */
 enum {
     DQN_PARAMS_ONLINE = 0,   /* theta                                   */
@@ -235,6 +238,56 @@ int replay_sample_gather(replay* rb, int32_t B, uint64_t sample_step, const int6
  * sample_stream must be ctx's train_stream.  Errors: those of the two calls. */
 int dqn_train_step_sampled(dqn_ctx* ctx, replay* rb, int32_t B, uint64_t sample_step,
                            int32_t prefetch_next, float* loss_out);
+
+/* ---- 8-bit levels and their product ----------------------------------------------------------- */
+
+/* The calls of this section and the next belong to no handle: they run on `stream`, which must belong to the current device (as must
+ * every buffer), use no memory but what they are given and may be captured into a graph.  Matrices are rows of contiguous elements;
+ * ldx, ldq, ... are row pitches in elements, at least a row long; a pointer needs the alignment of its elements only (rows that start on
+ * 16-byte borders are read and written faster).  What lies behind the last column or row is neither read nor written.  Outputs must not
+ * overlap inputs or each other. */
+
+/* Row r of x [rows, cols] as levels -127..127 with one scale: a = max_c |x_c|, scale = a / 127 rounded to fp32,
+ *   q_c = the whole number nearest to 127 x_c / a (the exact quotient; ties to even),
+ * and, if values != NULL, values_c = q_c * scale rounded to fp32 (at most its largest number) and then to x's type: what the levels stand for.  q or values may be NULL, not both.
+ * A row of zeros (or cols = 0) has scale 0 and levels 0; a row that holds a NaN or an infinity has scale NaN and levels 0, so that
+ * whatever is computed from it is NaN.  Errors: DQN_EINVAL (type, sizes outside 0..4194304 rows and 0..2^31-1 columns, a pitch shorter
+ * than a row, null / misaligned pointer). */
+#define Q8_QUANTIZE_MAX_ROWS 4194304
+int q8_quantize_rows(const void* x, int32_t type, int64_t ldx, int64_t rows, int64_t cols, int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv,
+                     void* stream);
+
+/* y_mn = act(sx_m * sw_n * sum_k x_mk w_nk + bias_n), x [M,K] and w [N,K] levels (-128..127), sx [M] and sw [N] their rows' scales, bias [N]
+ * or NULL, act the identity or (relu != 0) max(., 0); y [M,N] of the given type.  The sum is exact (32-bit integers; K <= 131071), the rest is
+ * computed in fp64 and rounded to fp32 and then to y's type; NaN scales give NaN, also through the ReLU.  K = 0: the sum is 0.  Errors: DQN_EINVAL (type,
+ * M or N outside 0..524288, K outside 0..131071, a pitch shorter than a row, null / misaligned pointer). */
+#define Q8_LINEAR_MAX_ROWS 524288
+#define Q8_LINEAR_MAX_K 131071
+int q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, int64_t ldw, const float* sw, const float* bias, int32_t relu, int64_t M,
+              int64_t N, int64_t K, void* y, int32_t type, int64_t ldy, void* stream);
+
+/* ---- drawing from a row of scores -------------------------------------------------------------- */
+
+/* One index per row of scores [rows, n] (Q values, logits): with m the row's maximum and w_i = exp((x_i - m) / T),
+ *   top_k   keeps the k entries that come first in the order (score descending, index ascending);            off: k <= 0 or k >= n
+ *   top_p   of these keeps the entries that have less than p * (the mass of these) before them in that order, the first one always; off: p >= 1
+ *   min_p   of these keeps the entries with w_i >= min(min_p, 1);                                            off: min_p <= 0
+ * and the index drawn is the lowest i at which the kept mass of indices 0..i exceeds u * (all kept mass).  logp_i = log(w_i / kept mass) is
+ * the logarithm of the probability it was drawn with.  T = 0: the lowest index of the maximum, logp 0.
+ *   temperature, top_k, top_p, min_p [rows] on the device, each or NULL (1, off, off, off);  u [rows] float32, clamped to
+ *   [0, 1 - 2^-24];  index [rows] int32 out;  logp [rows] float32 out, or NULL.
+ * Scores of -infinity are never drawn; scores of +infinity share the whole mass.  A row without a score above -infinity (n = 0 among them),
+ * one that holds a NaN, a temperature that is negative or not finite, or a NaN in top_p, min_p or u gives index -1 and logp NaN.
+ * Weights are held as whole multiples of 2^-40 of the largest, from fp64 exponentials: sums do not depend on their order, and the result is the
+ * same on every run.
+ * work: device memory of at least policy_sample_workspace(rows, n) bytes (NULL where that is 0), 16-byte aligned; it needs no
+ * clearing, and two calls that may overlap in time (on two streams, or in two graphs) need one each.  Errors: DQN_EINVAL (type, rows outside
+ * 0..4194304, n outside 0..4194304, ld < n, null / misaligned pointer, work too small). */
+#define POLICY_SAMPLE_MAX_ROWS 4194304
+#define POLICY_SAMPLE_MAX_N 4194304
+size_t policy_sample_workspace(int64_t rows, int64_t n);
+int policy_sample(const void* scores, int32_t type, int64_t ld, int64_t rows, int64_t n, const float* temperature, const int32_t* top_k, const float* top_p,
+                  const float* min_p, const float* u, int32_t* index, float* logp, void* work, size_t work_bytes, void* stream);
 
 /* ---- seeded synthetic inputs (benchmark support; stands in for emulator output) ----------- */
 

@@ -20,7 +20,10 @@ LIB_PATH = os.path.join(HERE, "libdqn_mi355.so")
 
 DQN_OK, DQN_EINVAL, DQN_EHIP, DQN_ENOMEM, DQN_ESTATE = 0, -1, -2, -3, -4
 DQN_PRECISION_FP32, DQN_PRECISION_BF16 = 0, 1
+DQN_TYPE_FP32, DQN_TYPE_BF16, DQN_TYPE_FP16 = 0, 1, 2
 DQN_ACT_STATIC_MAX_ENVS = 32
+Q8_QUANTIZE_MAX_ROWS, Q8_LINEAR_MAX_ROWS, Q8_LINEAR_MAX_K = 4194304, 524288, 131071
+POLICY_SAMPLE_MAX_ROWS = POLICY_SAMPLE_MAX_N = 4194304
 DQN_PARAMS_ONLINE, DQN_PARAMS_TARGET, DQN_PARAMS_RMS_V, DQN_PARAMS_RMS_M, DQN_PARAMS_GRAD = range(5)
 
 
@@ -76,6 +79,13 @@ EXPORTS = {
     "replay_num_valid": (C.c_int64, [C.c_void_p]),
     "replay_sample_gather": (C.c_int, [C.c_void_p, C.c_int32, C.c_uint64, C.c_void_p, C.c_void_p,
                                        C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "q8_quantize_rows": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                   C.c_void_p, C.c_int64, C.c_void_p]),
+    "q8_linear": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32,
+                            C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]),
+    "policy_sample_workspace": (C.c_size_t, [C.c_int64, C.c_int64]),
+    "policy_sample": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),
     "synth_frames": (C.c_int, [C.c_void_p, C.c_int64, C.c_uint64, C.c_uint64, C.c_uint64, C.c_uint32,
                                C.c_uint32, C.c_uint32, C.c_void_p]),
     "synth_transitions": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_uint64,
@@ -123,6 +133,26 @@ def _ptr(t):
     if t is None:
         return None
     assert t.is_contiguous(), "tensors handed to the library must be contiguous"
+    return t.data_ptr()
+
+
+_TYPES = {torch.float32: DQN_TYPE_FP32, torch.bfloat16: DQN_TYPE_BF16, torch.float16: DQN_TYPE_FP16}
+
+
+def _rows(t, dtype=None):
+    """Matrix whose rows are contiguous (its pitch is an argument of its own) -> address, None -> NULL."""
+    if t is None:
+        return None
+    assert t.shape[-1] <= 1 or t.stride(-1) == 1, "rows of a matrix handed to the library must be contiguous"
+    assert dtype is None or t.dtype is dtype or _TYPES.get(t.dtype) == dtype, "a matrix has another element type"
+    return t.data_ptr()
+
+
+def _vec(t, dtype):
+    """Contiguous array of the given element type -> address, None -> NULL."""
+    if t is None:
+        return None
+    assert t.dtype is dtype and t.is_contiguous(), "an array has another element type or is not contiguous"
     return t.data_ptr()
 
 
@@ -230,6 +260,27 @@ def replay_num_valid(rb):
 def replay_sample_gather(rb, B, sample_step, idx_in, s, s2, a, r, done, idx_out=None):
     _check(_lib.replay_sample_gather(rb, B, sample_step, _ptr(idx_in), _ptr(s), _ptr(s2), _ptr(a),
                                      _ptr(r), _ptr(done), _ptr(idx_out)))
+
+
+def q8_quantize_rows(x, type, ldx, rows, cols, q, ldq, scale, values, ldv, stream):
+    _check(_lib.q8_quantize_rows(_rows(x, type), type, ldx, rows, cols, _rows(q, torch.int8), ldq, _vec(scale, torch.float32),
+                                 _rows(values, type), ldv, _stream(stream)))
+
+
+def q8_linear(x, ldx, sx, w, ldw, sw, bias, relu, M, N, K, y, type, ldy, stream):
+    _check(_lib.q8_linear(_rows(x, torch.int8), ldx, _vec(sx, torch.float32), _rows(w, torch.int8), ldw, _vec(sw, torch.float32),
+                          _vec(bias, torch.float32), relu, M, N, K, _rows(y, type), type, ldy, _stream(stream)))
+
+
+def policy_sample_workspace(rows, n):
+    return int(_lib.policy_sample_workspace(rows, n))
+
+
+def policy_sample(scores, type, ld, rows, n, temperature, top_k, top_p, min_p, u, index, logp, work, work_bytes, stream):
+    f32 = torch.float32
+    _check(_lib.policy_sample(_rows(scores, type), type, ld, rows, n, _vec(temperature, f32), _vec(top_k, torch.int32),
+                              _vec(top_p, f32), _vec(min_p, f32), _vec(u, f32), _vec(index, torch.int32), _vec(logp, f32),
+                              _ptr(work), work_bytes, _stream(stream)))
 
 
 def synth_frames(dst, n, id0, id_step, seed, stream_tag, pix_threshold, background, stream):

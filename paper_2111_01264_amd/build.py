@@ -9,7 +9,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdqn_mi355.so")
-SOURCES = ["error.hip", "replay.hip", "net.hip", "envs.hip", "alg1.hip"]
+SOURCES = ["error.hip", "replay.hip", "net.hip", "envs.hip", "alg1.hip", "quant.hip", "policy.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument",
          # the first kernel arguments arrive in scalar registers with the wavefront instead of through a load from cold

@@ -30,7 +30,12 @@ int fail(int code, const char* fmt, ...);
                                __LINE__, hipGetErrorString(e__));                            \
     } while (0)
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+inline bool aligned16(const void* p) { return aligned_to(p, 16); }
+
+// Argument checks of the calls that belong to no handle: an element type; a stream of the current device (the launch goes there).
+int check_type(const char* who, int32_t type);
+int check_stream_device(const char* who, void* stream);
 
 // Replay internals needed by dqn_sync_target.
 int replay_flush_ordered(replay* rb);

@@ -1,4 +1,4 @@
-// Thread-local error message behind dqn_last_error().
+// Thread-local error message behind dqn_last_error(), and the argument checks that calls without a handle share.
 #include "common.h"
 
 namespace dqn {
@@ -16,6 +16,23 @@ int fail(int code, const char* fmt, ...)
     vsnprintf(error_buffer(), 512, fmt, ap);
     va_end(ap);
     return code;
+}
+
+int check_type(const char* who, int32_t type)
+{
+    if (type != DQN_TYPE_FP32 && type != DQN_TYPE_BF16 && type != DQN_TYPE_FP16) return fail(DQN_EINVAL, "%s: type %d", who, type);
+    return DQN_OK;
+}
+
+int check_stream_device(const char* who, void* stream)
+{
+    if (!stream) return DQN_OK;   // the null stream is the current device's
+    int current = -1;
+    hipDevice_t owner = -1;
+    DQN_HIP(hipGetDevice(&current));
+    DQN_HIP(hipStreamGetDevice(static_cast<hipStream_t>(stream), &owner));
+    if (owner != current) return fail(DQN_EINVAL, "%s: the stream belongs to device %d, the current device is %d", who, owner, current);
+    return DQN_OK;
 }
 
 }  // namespace dqn

@@ -41,5 +41,6 @@ __host__ __device__ inline Philox4 philox_draw(uint64_t seed, uint32_t tag, uint
 
 constexpr uint32_t kTagAct = 1;
 constexpr uint32_t kTagSample = 2;
+constexpr uint32_t kTagPolicy = 3;
 
 }  // namespace dqn

@@ -1,0 +1,147 @@
+"""q8_linear against the oracle in 64 bits, through the C boundary.  The sums are exact, so what is left are the roundings of the
+result: half a step of fp32, half a step of y's type, and fp64's own."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+import paper_2111_01264_amd as P
+
+TYPES = {"fp32": (torch.float32, P.DQN_TYPE_FP32), "bf16": (torch.bfloat16, P.DQN_TYPE_BF16), "fp16": (torch.float16, P.DQN_TYPE_FP16)}
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def levels(g, rows, ld, lo=-128):
+    return torch.randint(lo, 128, (rows, ld), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
+
+
+def wanted(x, K, sx, w, sw, bias, relu):
+    """In fp64 on the device: products and sums of whole numbers below 2^53 are exact."""
+    y = torch.matmul(x[:, :K].double(), w[:, :K].double().t().contiguous()) * torch.outer(sx.double(), sw.double())
+    if bias is not None:
+        y = y + bias.double()
+    return torch.where(y < 0, torch.zeros_like(y), y) if relu else y
+
+
+def check(y, want, dt):
+    y, finite = y.double(), torch.isfinite(want)
+    assert torch.equal(torch.isnan(y), torch.isnan(want))
+    eps, tiny = torch.finfo(dt).eps / 2, torch.finfo(dt).tiny * torch.finfo(dt).eps / 2
+    bound = want.abs() * (eps + 2.0 ** -24) * (1 + 2.0 ** -18) + tiny * (1 + 2.0 ** -18) + 2.0 ** -40 * want.abs().nan_to_num(0, 0, 0).max()
+    # (the last term: where sum and bias cancel, fp64's rounding of each, far below 2^-40 of the largest result)
+    assert torch.all(((y - want).abs() <= bound) | ~finite)
+
+
+def run(M, N, K, kind, relu=False, with_bias=True, pad=(0, 0, 0), off=0, stream=None, seed=0, lo=-128):
+    dt, code = TYPES[kind]
+    g = gen(seed + 7919 * M + 104729 * N + K)
+    ldx, ldw, ldy = K + pad[0], K + pad[1], N + pad[2]
+    xs, ws = levels(g, M * ldx + off + 64, 1, lo).view(-1), levels(g, N * ldw + off + 64, 1, lo).view(-1)
+    x, w = (t[off:off + r * ld].view(r, ld) if r * ld else t[:0].view(r, ld) for t, r, ld in ((xs, M, ldx), (ws, N, ldw)))
+    sx, sw = torch.rand(M, generator=g, device="cuda") * 0.02, torch.rand(N, generator=g, device="cuda") * 1e-3
+    if M > 2:
+        sx[1] = 0.0
+    bias = torch.randn(N, generator=g, device="cuda") * 0.1 if with_bias else None
+    y = torch.full((M + 1, ldy), 3.0, dtype=dt, device="cuda")
+    torch.cuda.synchronize()
+    P.q8_linear(x, ldx, sx, w, ldw, sw, bias, int(relu), M, N, K, y, code, ldy, stream)
+    torch.cuda.synchronize()
+    assert torch.all(y[M] == 3.0) and torch.all(y[:, N:] == 3.0)   # what lies behind stays as it was
+    check(y[:M, :N], wanted(x, K, sx, w, sw, bias, relu), dt)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 1, 64), (2, 3, 5), (1, 18, 512), (8, 18, 512), (8, 512, 3136), (16, 512, 3136), (17, 33, 100), (31, 64, 128), (33, 65, 129), (1, 1000, 4096),
+                                   (5, 2051, 777), (64, 64, 64), (64, 512, 3136), (65, 127, 255), (100, 300, 1000), (128, 128, 128), (129, 257, 513), (255, 256, 640), (256, 256, 256),
+                                   (257, 511, 1023), (300, 2051, 2003), (512, 512, 3136), (513, 1025, 96), (1000, 2000, 31), (700, 1536, 2048)])
+def test_sizes(kind, M, N, K):
+    run(M, N, K, kind)
+    run(M, N, K, kind, relu=True, with_bias=False, pad=((-K) % 16, (-K) % 16, 0))
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 40, 200), (20, 70, 333), (90, 130, 500), (300, 280, 700), (600, 520, 1111)])
+def test_pitches_and_alignments(M, N, K):
+    for pad, off in (((0, 0, 3), 1), ((5, 16, 1), 0), ((16, 7, 0), 4), ((48, 32, 8), 16), ((-K % 16, -K % 16 + 16, 2), 8), ((-K % 16, -K % 16, 0), 3)):
+        run(M, N, K, "bf16", pad=pad, off=off, seed=off)
+    run(M, N, K, "fp32", pad=(1, 0, 1), off=2)
+    run(M, N, K, "fp16", pad=(0, 1, 0), off=5)
+
+
+@pytest.mark.parametrize("M,N", [(1, 7), (40, 100), (300, 300)])
+def test_longest_sums_stay_exact(M, N):
+    """K at its limit with all levels -128: the sum is 2^31 - 2^14, the largest there is."""
+    K = P.Q8_LINEAR_MAX_K
+    x, w = (torch.full((r, K), -128, dtype=torch.int8, device="cuda") for r in (M, N))
+    one = lambda r: torch.ones(r, device="cuda")  # noqa: E731
+    y = torch.zeros(M, N, device="cuda")
+    P.q8_linear(x, K, one(M), w, K, one(N), None, 0, M, N, K, y, P.DQN_TYPE_FP32, N, None)
+    torch.cuda.synchronize()
+    assert torch.all(y.double() == float(np.float32(16384 * K)))
+
+
+def test_scales_at_the_ends_and_nan():
+    M, N, K = 4, 20, 130
+    g = gen(3)
+    x, w = levels(g, M, K), levels(g, N, K)
+    sx, sw = torch.tensor([1e-30, 1e30, float("nan"), 2e36], device="cuda"), torch.full((N,), 1e-30, device="cuda")
+    sw[1], sw[2] = float("nan"), 0.0
+    for relu in (0, 1):
+        y = torch.zeros(M, N, device="cuda")
+        P.q8_linear(x, K, sx, w, K, sw, None, relu, M, N, K, y, P.DQN_TYPE_FP32, N, None)
+        torch.cuda.synchronize()
+        want = wanted(x, K, sx, w, sw, None, relu)
+        assert torch.equal(torch.isnan(y.double()), torch.isnan(want))
+        fine = torch.isfinite(want)
+        assert torch.all((y.double() - want).abs()[fine] <= want.abs()[fine] * 2.0 ** -23 + 2.0 ** -150)
+
+
+def test_no_levels_leave_the_bias():
+    for M, N in ((2, 37), (300, 70)):
+        b = torch.randn(N, device="cuda")
+        y = torch.zeros(M, N, device="cuda")
+        s = torch.ones(max(M, N), device="cuda")
+        P.q8_linear(None, 0, s[:M], None, 0, s[:N], b, 1, M, N, 0, y, P.DQN_TYPE_FP32, N, None)
+        torch.cuda.synchronize()
+        assert torch.equal(y, torch.clamp_min(b, 0).expand(M, N))
+
+
+def test_another_stream_and_a_replayed_graph():
+    stream = torch.cuda.Stream()
+    run(8, 512, 3136, "fp32", relu=True, stream=stream)
+    run(300, 512, 3136, "bf16", stream=stream)
+    for M, N, K in ((4, 96, 500), (200, 384, 640)):
+        g = gen(8)
+        x, w = levels(g, M, K), levels(g, N, K)
+        sx, sw = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+        y = torch.zeros(M, N, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            P.q8_linear(x, K, sx, w, K, sw, None, 0, M, N, K, y, P.DQN_TYPE_FP32, N, stream)
+        for _ in range(3):
+            x.copy_(levels(g, M, K))
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            check(y, wanted(x, K, sx, w, sw, None, False), torch.float32)
+
+
+def test_rows_past_two_gigabytes():
+    """Offsets that pass 32 bits: a pitch of 2^20 levels and more than 2^12 rows."""
+    M, N, K, ld = 4100, 17, 100, 1 << 20
+    big = torch.empty(M * ld, dtype=torch.int8, device="cuda").view(M, ld)
+    g = gen(9)
+    big[:, :K] = levels(g, M, K)
+    w = levels(g, N, K)
+    s = torch.ones(M, device="cuda")
+    for x, lx, m, y_, ly, n in ((big, ld, M, w, K, N), (w, K, N, big, ld, M)):
+        y = torch.zeros(m, n, device="cuda")
+        P.q8_linear(x, lx, s[:m], y_, ly, s[:n], None, 0, m, n, K, y, P.DQN_TYPE_FP32, n, None)
+        torch.cuda.synchronize()
+        check(y, wanted(x, K, s[:m], y_, s[:n], None, False), torch.float32)
