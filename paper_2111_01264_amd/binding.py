@@ -136,23 +136,27 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_TYPES = {torch.float32: DQN_TYPE_FP32, torch.bfloat16: DQN_TYPE_BF16, torch.float16: DQN_TYPE_FP16}
+_TYPES = (torch.float32, torch.bfloat16, torch.float16)   # by DQN_TYPE_*
 
 
-def _rows(t, dtype=None):
-    """Matrix whose rows are contiguous (its pitch is an argument of its own) -> address, None -> NULL."""
+def _rows(t, dtype):
+    """Matrix of the given element type whose rows are contiguous (its pitch is an argument of its own) -> address, None -> NULL."""
     if t is None:
         return None
-    assert t.shape[-1] <= 1 or t.stride(-1) == 1, "rows of a matrix handed to the library must be contiguous"
-    assert dtype is None or t.dtype is dtype or _TYPES.get(t.dtype) == dtype, "a matrix has another element type"
+    assert t.dtype is dtype and (t.is_contiguous() or t.stride(-1) == 1), \
+        "a matrix handed to the library has another element type, or rows that are not contiguous"
     return t.data_ptr()
+
+
+def _typed(t, type):
+    return _rows(t, _TYPES[type]) if 0 <= type < len(_TYPES) else _rows(t, None if t is None else t.dtype)
 
 
 def _vec(t, dtype):
     """Contiguous array of the given element type -> address, None -> NULL."""
     if t is None:
         return None
-    assert t.dtype is dtype and t.is_contiguous(), "an array has another element type or is not contiguous"
+    assert t.dtype is dtype and t.is_contiguous(), "an array handed to the library has another element type or is not contiguous"
     return t.data_ptr()
 
 
@@ -263,13 +267,13 @@ def replay_sample_gather(rb, B, sample_step, idx_in, s, s2, a, r, done, idx_out=
 
 
 def q8_quantize_rows(x, type, ldx, rows, cols, q, ldq, scale, values, ldv, stream):
-    _check(_lib.q8_quantize_rows(_rows(x, type), type, ldx, rows, cols, _rows(q, torch.int8), ldq, _vec(scale, torch.float32),
-                                 _rows(values, type), ldv, _stream(stream)))
+    _check(_lib.q8_quantize_rows(_typed(x, type), type, ldx, rows, cols, _rows(q, torch.int8), ldq, _vec(scale, torch.float32),
+                                 _typed(values, type), ldv, _stream(stream)))
 
 
 def q8_linear(x, ldx, sx, w, ldw, sw, bias, relu, M, N, K, y, type, ldy, stream):
     _check(_lib.q8_linear(_rows(x, torch.int8), ldx, _vec(sx, torch.float32), _rows(w, torch.int8), ldw, _vec(sw, torch.float32),
-                          _vec(bias, torch.float32), relu, M, N, K, _rows(y, type), type, ldy, _stream(stream)))
+                          _vec(bias, torch.float32), relu, M, N, K, _typed(y, type), type, ldy, _stream(stream)))
 
 
 def policy_sample_workspace(rows, n):
@@ -278,7 +282,7 @@ def policy_sample_workspace(rows, n):
 
 def policy_sample(scores, type, ld, rows, n, temperature, top_k, top_p, min_p, u, index, logp, work, work_bytes, stream):
     f32 = torch.float32
-    _check(_lib.policy_sample(_rows(scores, type), type, ld, rows, n, _vec(temperature, f32), _vec(top_k, torch.int32),
+    _check(_lib.policy_sample(_typed(scores, type), type, ld, rows, n, _vec(temperature, f32), _vec(top_k, torch.int32),
                               _vec(top_p, f32), _vec(min_p, f32), _vec(u, f32), _vec(index, torch.int32), _vec(logp, f32),
                               _ptr(work), work_bytes, _stream(stream)))
 

@@ -1,4 +1,7 @@
 // 8-bit levels with a scale for each row, and the product of two such matrices (include/dqn_mi355.h: q8_quantize_rows, q8_linear).
+#include <mutex>
+#include <type_traits>
+
 #include "quant.h"
 
 #include "gemm_mfma.h"
@@ -45,40 +48,120 @@ __device__ inline float level_value(int q, float s)
     return v > 0x1.fffffep127f ? 0x1.fffffep127f : v < -0x1.fffffep127f ? -0x1.fffffep127f : v;   // (a NaN stays)
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const T* x, int64_t ldx, int64_t cols, int8_t* q, int64_t ldq, float* scale, T* values, int64_t ldv)
+template <typename T> struct Vec16 {   // 16 bytes of a row, at any alignment that its elements have
+    static constexpr int E = 16 / sizeof(T);
+    typedef T type __attribute__((ext_vector_type(E), aligned(sizeof(T))));
+    typedef int8_t levels __attribute__((ext_vector_type(E), aligned(1)));
+};
+
+struct QuantArgs { const void* x; int8_t* q; float* scale; void* values; int64_t ldx, ldq, ldv; int64_t rows; int cols; };
+
+template <typename T> __device__ inline uint32_t magnitude(T v) { return __float_as_uint(fabsf(static_cast<float>(v))); }   // they order as the values do, infinities and NaN above all others
+
+// Memory bounds it, so a row is read once: TPR threads hold it, R vectors of 16 bytes each, find its largest magnitude and write the levels.
+// A row beyond TPR * R vectors (R = 0) is read twice, the second time from cache.
+template <typename T, int TPR, int R>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void quantize_rows_kernel(QuantArgs a)
 {
-    __shared__ uint32_t part[4];
-    const int64_t row = blockIdx.x;
-    x += row * ldx;
-    uint32_t top = 0;   // bits of |x|: they order as the values do, infinities and NaN above all others
-    for (int64_t c = threadIdx.x; c < cols; c += 256) top = max(top, __float_as_uint(fabsf(static_cast<float>(x[c]))));
-    for (int d = 32; d; d >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), d)));
-    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = top;
-    __syncthreads();
-    top = max(max(part[0], part[1]), max(part[2], part[3]));
-    const bool finite = top < 0x7F800000u;
-    const float a = finite ? __uint_as_float(top) : 0.f, s = finite ? row_scale(a) : __uint_as_float(0x7FC00000u);
-    const Levels l = make_levels(a);
-    for (int64_t c = threadIdx.x; c < cols; c += 256) {
-        const int v = finite ? level_of(l, static_cast<float>(x[c])) : 0;
-        if (q) q[row * ldq + c] = static_cast<int8_t>(v);
-        if (values) values[row * ldv + c] = static_cast<T>(level_value(v, s));
+    typedef typename Vec16<T>::type vec;
+    typedef typename Vec16<T>::levels vec_q;
+    constexpr int E = Vec16<T>::E, RPB = TPR < 256 ? 256 / TPR : 1;   // rows per workgroup
+    const int64_t row = blockIdx.x * static_cast<int64_t>(RPB) + threadIdx.x / TPR;
+    if (TPR < 256 && row >= a.rows) return;   // (a wavefront's row, and no barrier below)
+    const int t = threadIdx.x % TPR, cols = a.cols, vecs = (cols + E - 1) / E;
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    auto load = [&](int v) {   // zeros behind the end
+        vec w;
+        if ((v + 1) * E <= cols) w = *reinterpret_cast<const vec*>(x + v * E);
+        else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) w[e] = v * E + e < cols ? x[v * E + e] : static_cast<T>(0.f);
+        }
+        return w;
+    };
+    uint32_t top = 0;
+    vec held[R ? R : 1];
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i * TPR + t < vecs) held[i] = load(i * TPR + t);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i * TPR + t < vecs) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) top = max(top, magnitude(held[i][e]));
+            }
+    } else {
+        for (int v = t; v < vecs; v += TPR) {
+            const vec w = load(v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) top = max(top, magnitude(w[e]));
+        }
     }
-    if (threadIdx.x == 0) scale[row] = s;
+#pragma unroll
+    for (int d = 32; d; d >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), d)));
+    if constexpr (TPR > 64) {
+        __shared__ uint32_t part[TPR / 64];
+        if ((t & 63) == 0) part[t >> 6] = top;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TPR / 64; ++i) top = max(top, part[i]);
+    }
+    const bool finite = top < 0x7F800000u;
+    const float m = finite ? __uint_as_float(top) : 0.f, s = finite ? row_scale(m) : __uint_as_float(0x7FC00000u);
+    const Levels l = make_levels(m);
+    int8_t* q = a.q ? a.q + row * a.ldq : nullptr;
+    T* values = a.values ? static_cast<T*>(a.values) + row * a.ldv : nullptr;
+    auto write = [&](int v, const vec& w) {
+        vec_q lev;
+        vec val;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int n = finite ? level_of(l, static_cast<float>(w[e])) : 0;
+            lev[e] = static_cast<int8_t>(n);
+            val[e] = static_cast<T>(level_value(n, s));
+        }
+        if ((v + 1) * E <= cols) {
+            if (q) *reinterpret_cast<vec_q*>(q + v * E) = lev;
+            if (values) *reinterpret_cast<vec*>(values + v * E) = val;
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (v * E + e < cols) {
+                    if (q) q[v * E + e] = lev[e];
+                    if (values) values[v * E + e] = val[e];
+                }
+        }
+    };
+    if constexpr (R > 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (i * TPR + t < vecs) write(i * TPR + t, held[i]);
+    } else {
+        for (int v = t; v < vecs; v += TPR) write(v, load(v));
+    }
+    if (t == 0) a.scale[row] = s;
 }
 
-template <typename T>
-static void launch_quantize(const void* x, int64_t ldx, int64_t rows, int64_t cols, int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv, hipStream_t st)
+template <typename T> static void launch_quantize(const QuantArgs& a, hipStream_t st)
 {
-    hipLaunchKernelGGL(quantize_rows_kernel<T>, dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, static_cast<const T*>(x), ldx, cols, q, ldq, scale, static_cast<T*>(values), ldv);
+    const int vecs = (a.cols + Vec16<T>::E - 1) / Vec16<T>::E;
+    const auto go = [&](auto kern, int tpr) {
+        const int rpb = tpr < 256 ? 256 / tpr : 1;
+        hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.rows + rpb - 1) / rpb)), dim3(tpr < 256 ? 256 : tpr), 0, st, a);
+    };
+    if (vecs <= 64 * 2) go(quantize_rows_kernel<T, 64, 2>, 64);
+    else if (vecs <= 256 * 4) go(quantize_rows_kernel<T, 256, 4>, 256);
+    else if (vecs <= 256 * 8) go(quantize_rows_kernel<T, 256, 8>, 256);
+    else if (vecs <= 1024 * 8) go(quantize_rows_kernel<T, 1024, 8>, 1024);
+    else go(quantize_rows_kernel<T, 1024, 0>, 1024);
 }
 
 int enqueue_quantize_rows(const void* x, int32_t type, int64_t ldx, int64_t rows, int64_t cols, int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv,
                           hipStream_t st)
 {
-    auto launch = type == DQN_TYPE_FP32 ? launch_quantize<float> : type == DQN_TYPE_BF16 ? launch_quantize<bf16_t> : launch_quantize<_Float16>;
-    launch(x, ldx, rows, cols, q, ldq, scale, values, ldv, st);
+    const QuantArgs a{x, q, scale, values, ldx, ldq, ldv, rows, static_cast<int>(cols)};
+    type == DQN_TYPE_FP32 ? launch_quantize<float>(a, st) : type == DQN_TYPE_BF16 ? launch_quantize<bf16_t>(a, st) : launch_quantize<_Float16>(a, st);
     DQN_LAUNCH_CHECK();
     return DQN_OK;
 }
@@ -96,11 +179,11 @@ struct Q8Args {
 };
 
 // The sum is exact in 32-bit integers; scales and bias are applied in fp64 (their product neither overflows nor underflows there, and
-// only the result is rounded) and the result is rounded once to y's type.
-template <typename T> __device__ inline T q8_result(int32_t acc, float sx, float sw, float b, bool relu)
+// only the result is rounded) and the result is rounded to fp32 and to y's type.  floor: 0 with a ReLU, else -infinity; a NaN stays.
+template <typename T> __device__ inline T q8_result(int32_t acc, float sx, float sw, float b, float floor)
 {
     const float v = static_cast<float>(static_cast<double>(acc) * (static_cast<double>(sx) * static_cast<double>(sw)) + static_cast<double>(b));
-    return static_cast<T>(relu && v < 0.f ? 0.f : v);   // (a NaN stays)
+    return static_cast<T>(v < floor ? floor : v);
 }
 
 // 16 levels of a row from column k on; zeros from column K on and for rows that there are none of.
@@ -119,33 +202,305 @@ __device__ inline i32x4 q8_load(const int8_t* row, int k, int K, bool in)
     return v;
 }
 
-template <typename T>
-__global__ __launch_bounds__(256) void q8_linear_kernel(Q8Args a)
+// The 32x32 matrix instruction on 8-bit operands (the 16x16 one alike): lane l feeds row l % 32 with 16 levels of k, the lanes below 32 and the others
+// with different ones, and receives column l % 32 with rows 8 (v / 4) + 4 (l / 32) + v % 4, v = 0 .. 15.  Which 16 of a tile's k a lane
+// feeds is free as long as both operands agree.  w is the first operand everywhere, so that a lane holds one row m of y and four columns n in a row.
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+__device__ inline i32x16 q8_mma(const i32x4& w, const i32x4& x, const i32x16& acc) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(w, x, acc, 0, 0, 0); }
+__device__ inline i32x4 q8_mma(const i32x4& w, const i32x4& x, const i32x4& acc) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0); }
+
+// Four columns n .. n + 3 of y as they leave the matrix instructions: their scales and biases once, then the rows m that this lane has of them.
+struct Q8Columns {
+    float sw[4], b[4], floor;
+    int n, left;   // columns of them that there are
+};
+__device__ inline Q8Columns q8_columns(const Q8Args& a, int n)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int m0 = static_cast<int>(blockIdx.y) * 16, n0 = (static_cast<int>(blockIdx.x) * 4 + wave) * 16, r = lane & 15, kq = 16 * (lane >> 4);
-    const bool in_m = m0 + r < a.M, in_n = n0 + r < a.N;
-    const int8_t* x = a.x + static_cast<int64_t>(in_m ? m0 + r : 0) * a.ldx;
-    const int8_t* w = a.w + static_cast<int64_t>(in_n ? n0 + r : 0) * a.ldw;
-    i32x4 acc = {0, 0, 0, 0};
-    for (int k = 0; k < a.K; k += 64) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(q8_load(x, k + kq, a.K, in_m), q8_load(w, k + kq, a.K, in_n), acc, 0, 0, 0);
-    if (!in_n) return;
-    const float sw = a.sw[n0 + r], b = a.bias ? a.bias[n0 + r] : 0.f;
+    Q8Columns c;
+    c.n = n; c.left = a.N - n;
+    c.floor = a.relu ? 0.f : -INFINITY;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int m = m0 + 4 * (lane >> 4) + i;
-        if (m < a.M) static_cast<T*>(a.y)[m * a.ldy + n0 + r] = q8_result<T>(acc[i], a.sx[m], sw, b, a.relu);
+        const int at = min(n + i, a.N - 1);
+        c.sw[i] = a.sw[at];
+        c.b[i] = a.bias ? a.bias[at] : 0.f;
     }
+    return c;
+}
+template <typename T> __device__ inline void q8_store(const Q8Args& a, const Q8Columns& c, int m, float sx, int32_t v0, int32_t v1, int32_t v2, int32_t v3)
+{
+    typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const int32_t v[4] = {v0, v1, v2, v3};
+    T4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = q8_result<T>(v[i], sx, c.sw[i], c.b[i], c.floor);
+    if (m >= a.M) return;
+    T* y = static_cast<T*>(a.y) + m * a.ldy + c.n;
+    if (c.left >= 4) *reinterpret_cast<T4*>(y) = out;
+    else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < c.left) y[i] = out[i];
+    }
+}
+
+// ---- few rows: the weights are streamed once, from memory straight into the matrix instructions ---------------------------------
+//
+// A workgroup owns BN rows of w and all of MT * BN rows of x (BN = 16: at most 64 rows of x; BN = 32: one tile of 32 of them per
+// workgroup); its wavefronts take every WAVES-th stretch of k and meet in LDS at the end.  No staging: a row of w is used by one
+// wavefront only, and the rows of x come from cache.
+template <typename T, int BN, int MT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void q8_stream_kernel(Q8Args a)
+{
+    typedef typename std::conditional<BN == 16, i32x4, i32x16>::type acc_t;
+    constexpr int KI = BN == 16 ? 64 : 32, V = BN == 16 ? 4 : 16;   // k of one instruction, results per lane
+    constexpr int U = BN == 16 ? (MT == 1 ? 8 : 4) : 4;             // instructions' worth of w in flight per wavefront
+    __shared__ int32_t part[WAVES > 1 ? (WAVES - 1) * MT * V * 64 : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = static_cast<int>(blockIdx.x) * BN, m0 = static_cast<int>(blockIdx.y) * (MT * BN), r = lane % BN, kq = 16 * (lane / BN);
+    const int8_t* w = a.w + static_cast<int64_t>(min(n0 + r, a.N - 1)) * a.ldw;   // (rows past the end repeat the last one: their results are not stored)
+    const int8_t* x[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) x[t] = a.x + static_cast<int64_t>(min(m0 + t * BN + r, a.M - 1)) * a.ldx;
+    acc_t acc[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+        for (int v = 0; v < V; ++v) acc[t][v] = 0;
+    const int K = a.K, whole = K / (KI * U);   // stretches of KI * U
+    for (int s = wave; s < whole; s += WAVES) {
+        const int k = s * (KI * U) + kq;
+        i32x4 wf[U], xf[MT][U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) __builtin_memcpy(&wf[u], w + k + u * KI, 16);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) __builtin_memcpy(&xf[t][u], x[t] + k + u * KI, 16);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) acc[t] = q8_mma(wf[u], xf[t][u], acc[t]);
+    }
+    for (int k = whole * (KI * U) + wave * KI; k < K; k += WAVES * KI) {   // the rest, in single instructions
+        const i32x4 wf = q8_load(w, k + kq, K, true);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) acc[t] = q8_mma(wf, q8_load(x[t], k + kq, K, true), acc[t]);
+    }
+    if constexpr (WAVES > 1) {
+        if (wave > 0) {
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int v = 0; v < V; ++v) part[((wave - 1) * MT * V + t * V + v) * 64 + lane] = acc[t][v];
+        }
+        __syncthreads();
+        if (wave > 0) return;
+#pragma unroll
+        for (int q = 0; q < WAVES - 1; ++q)
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int v = 0; v < V; ++v) acc[t][v] += part[(q * MT * V + t * V + v) * 64 + lane];
+    }
+#pragma unroll
+    for (int g = 0; g < V / 4; ++g) {
+        const Q8Columns c = q8_columns(a, n0 + (BN == 16 ? 4 * (lane / BN) : 8 * g + 4 * (lane / BN)));
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int m = m0 + t * BN + r;
+            q8_store<T>(a, c, m, a.sx[min(m, a.M - 1)], acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]);
+        }
+    }
+}
+
+// ---- many rows: tiles staged through LDS -----------------------------------------------------------------------------------
+//
+// 256 threads own a TILE x TILE piece of y, each of the four wavefronts a quarter (two by two).  k advances in steps of 64: a stage holds 64
+// levels of TILE rows of x and of w, kStages of them are in LDS, and the loads of a step are issued kStages - 1 steps ahead, straight from
+// memory into LDS.  A wavefront reads the operands of the next half step while it multiplies those of this one; there is one barrier
+// per step, in the middle: behind it the stage that everybody has read is free, and the next one is complete.
+//
+// A row's four 16-byte chunks are stored at the places c ^ swizzle(row), so that the 32 rows that one read takes the same chunk of do
+// not meet in the same banks.
+constexpr int kStep = 64, kStages = 4;
+__device__ inline int q8_swizzle(int row) { return (((row >> 1) ^ (row >> 3)) & 1) | ((row >> 1) & 2); }
+
+// 16 bytes per lane from base + offset (which differs per lane) into LDS at the wavefront's `lds` + 16 * lane.  Nothing but q8_wait waits for them.
+__device__ inline void q8_to_lds(const int8_t* base, uint32_t offset, uint32_t lds)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + offset), (__attribute__((address_space(3))) void*)static_cast<uintptr_t>(lds), 16, 0, 0);
+}
+template <int LEFT> __device__ inline void q8_wait() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory"); }
+
+template <typename T, int TILE, bool ALIGNED>
+__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void q8_tile_kernel(Q8Args a, int tiles_m, int tiles_n)
+{
+    constexpr int F = TILE / 64;                                   // 32-row operand tiles per wavefront and side
+    constexpr int kHalf = TILE * kStep, kStage = 2 * kHalf;        // bytes: w's rows, then x's
+    constexpr int L = kStage / 16 / 256;                           // 16-byte loads per thread and step
+    extern __shared__ __attribute__((aligned(128))) int8_t q8_smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes a contiguous eighth of the tiles, in strips of eight
+    // tile rows, so that the tiles that are worked on together share rows of x and w.
+    int tm, tn;
+    {
+        const uint32_t total = static_cast<uint32_t>(tiles_m) * tiles_n, id = blockIdx.x, per = total >> 3;
+        const uint32_t l = id < per * 8 ? (id & 7) * per + (id >> 3) : id;
+        const uint32_t strip = l / (8u * tiles_n), first = strip * 8, rows = min(8u, static_cast<uint32_t>(tiles_m) - first), in = l - strip * 8u * tiles_n;
+        tm = static_cast<int>(first + in % rows);
+        tn = static_cast<int>(in / rows);
+    }
+    const int m0 = tm * TILE, n0 = tn * TILE, K = a.K;
+    // this thread's chunks of a stage: rows (tid >> 2) + 64 j of w, then of x
+    const int row = tid >> 2, chunk = (tid & 3) ^ q8_swizzle(tid >> 2);
+    const int8_t* wb = a.w + static_cast<int64_t>(n0) * a.ldw;
+    const int8_t* xb = a.x + static_cast<int64_t>(m0) * a.ldx;
+    auto row_of = [&](int j) { return j < L / 2 ? min(row + 64 * j, a.N - 1 - n0) : min(row + 64 * (j - L / 2), a.M - 1 - m0); };   // (past the end: the last one again)
+    uint32_t offset[L];
+    const int8_t* ptr[L];
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+        if constexpr (ALIGNED) offset[j] = static_cast<uint32_t>(row_of(j)) * static_cast<uint32_t>(j < L / 2 ? a.ldw : a.ldx) + 16 * chunk;
+        else ptr[j] = j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx;
+    }
+    const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int8_t*)q8_smem));
+    auto request = [&](int step) {   // ALIGNED
+        const uint32_t to = lds0 + (step % kStages) * kStage + wave * 1024;
+#pragma unroll
+        for (int j = 0; j < L; ++j) q8_to_lds((j < L / 2 ? wb : xb) + static_cast<int64_t>(step) * kStep, offset[j], to + j * 4096);
+    };
+    i32x4 reg[ALIGNED ? 1 : L];
+    auto fetch = [&](int step) {   // not ALIGNED
+#pragma unroll
+        for (int j = 0; j < L; ++j) reg[j] = q8_load(ptr[j], step * kStep + 16 * chunk, K, true);
+    };
+    auto put = [&](int step) {
+#pragma unroll
+        for (int j = 0; j < L; ++j) *reinterpret_cast<i32x4*>(q8_smem + (step % kStages) * kStage + j * 4096 + tid * 16) = reg[j];
+    };
+    // reads: rows 32 i + lane % 32 of this wavefront's part, chunks 2 h and 2 h + 1
+    const int lr = lane & 31, lc = lane >> 5, wn = (wave & 1) * (TILE / 2), wm = (wave >> 1) * (TILE / 2);
+    const int sw = q8_swizzle(lr);
+    const int at_w = (wn + lr) * kStep, at_x = kHalf + (wm + lr) * kStep;
+    i32x4 wf[2][F], xf[2][F];
+    auto read = [&](int step, int h) {
+        const int8_t* st = q8_smem + (step % kStages) * kStage + 16 * ((2 * h + lc) ^ sw);
+#pragma unroll
+        for (int i = 0; i < F; ++i) wf[h][i] = *reinterpret_cast<const i32x4*>(st + at_w + i * 32 * kStep);
+#pragma unroll
+        for (int i = 0; i < F; ++i) xf[h][i] = *reinterpret_cast<const i32x4*>(st + at_x + i * 32 * kStep);
+    };
+    i32x16 acc[F][F];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int j = 0; j < F; ++j)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
+    auto multiply = [&](int h) {
+#pragma unroll
+        for (int i = 0; i < F; ++i)
+#pragma unroll
+            for (int j = 0; j < F; ++j) acc[i][j] = q8_mma(wf[h][i], xf[h][j], acc[i][j]);
+    };
+    // ALIGNED: whole steps through LDS directly, a last partial one through registers, which cut it off at K
+    const int steps = ALIGNED ? K / kStep : (K + kStep - 1) / kStep;
+    if (steps > 0) {
+        if constexpr (ALIGNED) {
+#pragma unroll
+            for (int s = 0; s < kStages; ++s)
+                if (s < steps) request(s);
+            if (steps >= kStages) q8_wait<(kStages - 1) * L>(); else q8_wait<0>();
+        } else {
+            for (int s = 0; s < kStages - 1; ++s)
+                if (s < steps) { fetch(s); put(s); }
+            if (kStages - 1 < steps) fetch(kStages - 1);
+            __syncthreads();
+        }
+        read(0, 0);
+        for (int s = 0; s < steps; ++s) {
+            read(s, 1);
+            multiply(0);
+            if (s + 1 < steps) {
+                if constexpr (ALIGNED) {
+                    if (s + kStages <= steps) q8_wait<(kStages - 2) * L>(); else q8_wait<0>();
+                    if (s + kStages < steps) request(s + kStages);
+                } else {
+                    if (s + kStages - 1 < steps) put(s + kStages - 1);
+                    __syncthreads();
+                    if (s + kStages < steps) fetch(s + kStages);
+                }
+                read(s + 1, 0);
+            }
+            multiply(1);
+        }
+    }
+    if (ALIGNED && steps * kStep < K) {
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < L; ++j) {
+            const int8_t* p = (j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx);
+            *reinterpret_cast<i32x4*>(q8_smem + j * 4096 + tid * 16) = q8_load(p, steps * kStep + 16 * chunk, K, true);
+        }
+        __syncthreads();
+        read(0, 0); read(0, 1);
+        multiply(0); multiply(1);
+    }
+    float sx[F];
+#pragma unroll
+    for (int j = 0; j < F; ++j) sx[j] = a.sx[min(m0 + wm + 32 * j + lr, a.M - 1)];
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const Q8Columns c = q8_columns(a, n0 + wn + 32 * i + 8 * g + 4 * lc);
+#pragma unroll
+            for (int j = 0; j < F; ++j)
+                q8_store<T>(a, c, m0 + wm + 32 * j + lr, sx[j], acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
+        }
+}
+
+template <typename T, int TILE, bool ALIGNED> static int launch_tile(const Q8Args& a, hipStream_t st)
+{
+    constexpr int smem = 2 * TILE * kStep * kStages;
+    static std::once_flag once;
+    static hipError_t raised = hipSuccess;
+    std::call_once(once, [] { raised = hipFuncSetAttribute(reinterpret_cast<const void*>(q8_tile_kernel<T, TILE, ALIGNED>), hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+    DQN_HIP(raised);
+    const int tm = (a.M + TILE - 1) / TILE, tn = (a.N + TILE - 1) / TILE;
+    hipLaunchKernelGGL((q8_tile_kernel<T, TILE, ALIGNED>), dim3(static_cast<unsigned>(tm) * tn), dim3(256), smem, st, a, tm, tn);
+    DQN_LAUNCH_CHECK();
+    return DQN_OK;
+}
+
+template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
+{
+    const auto blocks = [&](int bn, int bm) { return dim3(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + bm - 1) / bm)); };
+    if (a.M <= 64) {
+        if (a.M <= 16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 1, 4>), blocks(16, 16), dim3(256), 0, st, a);
+        else if (a.M <= 32) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 2, 4>), blocks(16, 32), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 64), dim3(256), 0, st, a);
+        DQN_LAUNCH_CHECK();
+        return DQN_OK;
+    }
+    const int64_t t256 = static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = static_cast<int64_t>((a.M + 127) / 128) * ((a.N + 127) / 128);
+    if (t128 < 64) {
+        hipLaunchKernelGGL((q8_stream_kernel<T, 32, 1, 4>), blocks(32, 32), dim3(256), 0, st, a);
+        DQN_LAUNCH_CHECK();
+        return DQN_OK;
+    }
+    // 16-byte loads straight into LDS need rows on 16-byte borders; a lane's place within a tile is a 32-bit offset
+    const bool aligned = aligned16(a.x) && aligned16(a.w) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.ldx < (1 << 23) && a.ldw < (1 << 23);
+    if (t256 >= 192) return aligned ? launch_tile<T, 256, true>(a, st) : launch_tile<T, 128, false>(a, st);
+    return aligned ? launch_tile<T, 128, true>(a, st) : launch_tile<T, 128, false>(a, st);
 }
 
 int enqueue_q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, int64_t ldw, const float* sw, const float* bias, bool relu, int64_t M,
                       int64_t N, int64_t K, void* y, int32_t type, int64_t ldy, hipStream_t st)
 {
-    Q8Args a{x, w, sx, sw, bias, y, ldx, ldw, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K), relu};
-    auto kern = type == DQN_TYPE_FP32 ? q8_linear_kernel<float> : type == DQN_TYPE_BF16 ? q8_linear_kernel<bf16_t> : q8_linear_kernel<_Float16>;
-    hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((N + 63) / 64), static_cast<unsigned>((M + 15) / 16)), dim3(256), 0, st, a);
-    DQN_LAUNCH_CHECK();
-    return DQN_OK;
+    const Q8Args a{x, w, sx, sw, bias, y, ldx, ldw, ldy, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K), relu};
+    return type == DQN_TYPE_FP32 ? launch_linear<float>(a, st) : type == DQN_TYPE_BF16 ? launch_linear<bf16_t>(a, st) : launch_linear<_Float16>(a, st);
 }
 
 }  // namespace dqn

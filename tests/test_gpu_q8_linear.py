@@ -59,7 +59,7 @@ def run(M, N, K, kind, relu=False, with_bias=True, pad=(0, 0, 0), off=0, stream=
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 1, 64), (2, 3, 5), (1, 18, 512), (8, 18, 512), (8, 512, 3136), (16, 512, 3136), (17, 33, 100), (31, 64, 128), (33, 65, 129), (1, 1000, 4096),
                                    (5, 2051, 777), (64, 64, 64), (64, 512, 3136), (65, 127, 255), (100, 300, 1000), (128, 128, 128), (129, 257, 513), (255, 256, 640), (256, 256, 256),
-                                   (257, 511, 1023), (300, 2051, 2003), (512, 512, 3136), (513, 1025, 96), (1000, 2000, 31), (700, 1536, 2048)])
+                                   (257, 511, 1023), (300, 2051, 2003), (512, 512, 3136), (513, 1025, 96), (1000, 2000, 31), (700, 1536, 2048), (3500, 4000, 200), (3585, 3329, 640), (200, 49000, 77)])
 def test_sizes(kind, M, N, K):
     run(M, N, K, kind)
     run(M, N, K, kind, relu=True, with_bias=False, pad=((-K) % 16, (-K) % 16, 0))
