@@ -42,30 +42,52 @@ __device__ inline uint64_t entry_of(float x, int index) { return static_cast<uin
 __device__ inline float entry_score(uint64_t e) { return key_score(static_cast<uint32_t>(e >> 32)); }
 __device__ inline int entry_index(uint64_t e) { return static_cast<int>(~static_cast<uint32_t>(e)); }
 
+// a * b + c with c in scalar registers: left to itself the compiler copies each coefficient into vector registers first, two more instructions for each.
+__device__ __forceinline__ double fma_s(double a, double b, double c)
+{
+    double r;
+    asm("v_fma_f64 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "s"(c));
+    return r;
+}
+template <typename T> __device__ __forceinline__ T uniform(T v)   // the same in every lane: into scalar registers
+{
+    constexpr int N = sizeof(T) / 4;
+    uint32_t w[N];
+    __builtin_memcpy(w, &v, sizeof(T));
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+    __builtin_memcpy(&v, w, sizeof(T));
+    return v;
+}
+
 struct Weights {
-    double m, c;   // the row's maximum, log2(e) / T
-    bool inf;      // m is +infinity: its equals have weight 1, all others 0
+    double m, c;   // the row's maximum, log2(e) / T.  Where the maximum is +infinity it counts as 10^39 and c as 10^300: its equals have weight 1, all others 0
     // 2^40 w before it is rounded to a whole number: 2^y = 2^i 2^f, |f| <= 1/2, the second factor by its Taylor series up to f^11 (off by less than 2^-46).
-    // Minus infinity and everything far below the maximum end as 2^-1060, which is 0 units.
+    // Minus infinity and everything far below the maximum end as 2^-960, which is 0 units.
     __device__ __forceinline__ double raw(float x) const
     {
-        if (inf) return x == INFINITY ? kUnits : 0.0;
         constexpr double L = 0.693147180559945309417232121458, L2 = L * L / 2, L3 = L2 * L / 3, L4 = L3 * L / 4, L5 = L4 * L / 5, L6 = L5 * L / 6, L7 = L6 * L / 7,
-                         L8 = L7 * L / 8, L9 = L8 * L / 9, L10 = L9 * L / 10, L11 = L10 * L / 11;
-        const double y = fmax((static_cast<double>(x) - m) * c, -1100.0), i = rint(y), f = y - i;
-        double v = L11;
-        v = fma(v, f, L10); v = fma(v, f, L9); v = fma(v, f, L8); v = fma(v, f, L7); v = fma(v, f, L6); v = fma(v, f, L5);
-        v = fma(v, f, L4); v = fma(v, f, L3); v = fma(v, f, L2); v = fma(v, f, L); v = fma(v, f, 1.0);
-        return ldexp(v, static_cast<int>(i) + 40);
+                         L8 = L7 * L / 8, L9 = L8 * L / 9, L10 = L9 * L / 10, L11 = L10 * L / 11, U = kUnits, kRound = 0x1.8p52;   // (adding kRound leaves the nearest whole number in the low bits)
+        const double y = fmax((fmin(static_cast<double>(x), 1e39) - m) * c, -1000.0), at = y + kRound, f = y - (at - kRound);
+        double v = fma_s(f, uniform(L11 * U), L10 * U);
+        v = fma_s(v, f, L9 * U); v = fma_s(v, f, L8 * U); v = fma_s(v, f, L7 * U); v = fma_s(v, f, L6 * U); v = fma_s(v, f, L5 * U);
+        v = fma_s(v, f, L4 * U); v = fma_s(v, f, L3 * U); v = fma_s(v, f, L2 * U); v = fma_s(v, f, L * U); v = fma_s(v, f, U);
+        const uint64_t bits = __builtin_bit_cast(uint64_t, v);
+        const uint32_t i = static_cast<uint32_t>(__builtin_bit_cast(uint64_t, at));
+        return __builtin_bit_cast(double, bits + (static_cast<uint64_t>(i << 20) << 32));
     }
-    __device__ double whole(float x) const { return rint(raw(x)); }   // (sums of up to 2^13 of them are exact in fp64; a thread has at most 2^12)
-    __device__ uint64_t units(float x) const { return static_cast<uint64_t>(whole(x)); }
+    __device__ __forceinline__ double whole(float x) const { return rint(raw(x)); }   // (sums of up to 2^13 of them are exact in fp64; a thread has at most 2^12)
+    __device__ __forceinline__ uint64_t units(float x) const { return whole_units(whole(x)); }
+    __device__ __forceinline__ static uint64_t whole_units(double w) { return __builtin_bit_cast(uint64_t, w + 0x1p52) - 0x4330000000000000ull; }   // a whole number below 2^52
 };
-__device__ inline Weights make_weights(float m, double t) { return Weights{m, 1.4426950408889634074 / t, m == INFINITY}; }
+__device__ inline Weights make_weights(float m, double t)
+{
+    return uniform(m == INFINITY ? Weights{1e39, 1e300} : Weights{m, 1.4426950408889634074 / t});
+}
 
 __device__ inline float log_probability(float x, const Weights& w, double t, uint64_t total)
 {
-    const double d = w.inf || static_cast<double>(x) == w.m ? 0.0 : (static_cast<double>(x) - w.m) / t;
+    const double d = x == INFINITY ? 0.0 : (static_cast<double>(x) - w.m) / t;
     return static_cast<float>(d - log(static_cast<double>(total) / kUnits));
 }
 __device__ inline void answer(const PolicyArgs& a, int64_t row, int32_t index, float logp)
@@ -138,27 +160,32 @@ __global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t
     if (lane == pick) answer(a, row, pick, log_probability(x, w, s.t, total));
 }
 
-// ---- a row by one workgroup -----------------------------------------------------------------------------------------------
+// ---- longer rows: what the kernels below share ------------------------------------------------------------------------------
 //
 // The kept set is a prefix of the filters' order cut by min-p, so all a filter has to find is its last entry (a score with its index).
-//   top-k with a small k   the k-th largest of 256 groups' maxima is a lower bound for the k-th largest score: the few entries from it on go into
+//   top-k with a small k   the k-th largest of some 256 groups' maxima is a lower bound for the k-th largest score: the few entries from it on go into
 //                          a list, which is sorted; everything else happens in the list.
-//   otherwise              a histogram of the scores that can matter over 2048 equal parts of their range finds the part in which the count
-//                          or the mass crosses; its entries go into the list.  Where they are too many (equal scores), the crossing is found digit by
-//                          digit in the scores' keys.
-// Every pass reads the row again, from cache: held in registers, it needs code without loops, of which the passes over 128 scores per thread took
-// 300 KB.  Wavefront w has a contiguous stretch of the row, so that the draw, a search in index order, goes from wavefront to lane to entry.
-constexpr int kBins = 2048, kList = 2048, kGroups = 256, kListK = 192;
+//   otherwise              a histogram (mass and, for top-k, entries) of the scores that have mass over BINS equal parts of their range finds the part
+//                          in which a count or a mass crosses; its entries go into the list, which is sorted.
+// Where the entries overflow the list (equal scores) or there is no range, the crossing is found digit by digit in the scores' keys.
+//
+// Every pass reads the scores again, from cache: held in registers, they need code without loops, of which the passes over 128 scores per thread took
+// 300 KB.  A wavefront has a contiguous stretch, so that the draw, a search in index order, goes from a quarter of such a stretch to one score.  What
+// bounds it are the exponentials: 25 instructions at fp64's rate for each.
+constexpr int kListK = 192, kPolicyGroups = 512;
 
-struct RowShared {
-    uint64_t bins[kBins];    // a histogram, or the sorted list
-    uint64_t list[kList];
+// (sized by the threads: four workgroups of 256 threads fit a compute unit)
+template <int THREADS> struct RowShared {
+    static constexpr int BINS = 2 * THREADS, LIST = 2 * THREADS;
+    alignas(16) uint64_t mass[BINS];   // the histogram
+    uint32_t entries[BINS];
+    alignas(16) uint64_t list[LIST];
+    uint64_t sorted[LIST];
     uint64_t part[16], part2[16];
-    uint32_t group[kGroups];
-    uint32_t count;          // entries in the list
+    alignas(16) uint32_t group[kPolicyGroups];
+    uint32_t count;             // entries in the list
     int pick;
     uint64_t pick_sum, bound;
-    double target;
 };
 
 template <typename T, int THREADS> struct Row {
@@ -166,8 +193,9 @@ template <typename T, int THREADS> struct Row {
     typedef T vec __attribute__((ext_vector_type(E), aligned(sizeof(T))));
     const T* x;
     int n, trips, lane, wave;
-    __device__ Row(const PolicyArgs& a, int64_t row)
-        : x(static_cast<const T*>(a.scores) + row * a.ld), n(a.n), trips(((a.n + E - 1) / E + THREADS - 1) / THREADS), lane(threadIdx.x & 63),
+    // the n scores of the row from `from` on; indices count from there
+    __device__ Row(const PolicyArgs& a, int64_t row, int from, int n_)
+        : x(static_cast<const T*>(a.scores) + row * a.ld + from), n(n_), trips(((n_ + E - 1) / E + THREADS - 1) / THREADS), lane(threadIdx.x & 63),
           wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6))
     {
     }
@@ -181,23 +209,41 @@ template <typename T, int THREADS> struct Row {
         for (int e = 0; e < E; ++e) v[e] = at + e < n ? x[at + e] : static_cast<T>(-INFINITY);
         return v;
     }
-    // f(index of the first, 16 bytes of scores) for the trips from `from` to `to`; behind the end they are -infinity
-    template <typename F> __device__ __forceinline__ void each(int from, int to, const F& f) const
+    // f(index of the first, 16 bytes of scores) for every trip; behind the end they are -infinity.  AHEAD loads are in flight: a pass that hardly
+    // computes waits for nothing else, one with exponentials has the other wavefronts to hide a single one.
+    template <int AHEAD, typename F> __device__ __forceinline__ void each(const F& f) const
     {
-        if (from >= to) return;
-        vec next = load(from);
+        if constexpr (AHEAD == 1) {
+            vec next = load(0);
 #pragma unroll 1
-        for (int i = from; i < to; ++i) {
-            const vec v = next;
-            if (i + 1 < to) next = load(i + 1);
-            f(first(i), v);
+            for (int i = 0; i < trips; ++i) {
+                const vec v = next;
+                if (i + 1 < trips) next = load(i + 1);
+                f(first(i), v);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < trips; i += AHEAD) {
+                vec v[AHEAD];
+#pragma unroll
+                for (int q = 0; q < AHEAD; ++q) v[q] = load(i + q);   // (behind the last trip: the next wavefront's scores, or -infinity; not used)
+#pragma unroll
+                for (int q = 0; q < AHEAD; ++q)
+                    if (i + q < trips) f(first(i + q), v[q]);
+            }
         }
     }
-    template <typename F> __device__ __forceinline__ void each(const F& f) const { each(0, trips, f); }
+    static __device__ __forceinline__ bool any(vec v, float bound)   // of the wavefront's scores is as large
+    {
+        bool a = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) a |= static_cast<float>(v[e]) >= bound;
+        return __any(a);
+    }
     // f(score, index)
     template <typename F> __device__ __forceinline__ void each_score(const F& f) const
     {
-        each([&](int at, const vec& v) {
+        each<1>([&](int at, const vec& v) {
 #pragma unroll
             for (int e = 0; e < E; ++e) f(static_cast<float>(v[e]), at + e);
         });
@@ -216,11 +262,11 @@ template <int WAVES> __device__ inline uint64_t block_sum(uint64_t* part, uint64
     return s;
 }
 
-// The first j of 0 .. kBins - 1 (each thread's are next to each other) at which above + f(0) + .. + f(j) reaches target, and the sum before it.  One
+// The first j of 0 .. BINS - 1 (each thread's are next to each other) at which above + f(0) + .. + f(j) reaches target, and the sum before it.  One
 // does, or sh.pick stays -1.
-template <int THREADS, typename F> __device__ __forceinline__ void first_reaching(RowShared& sh, const F& f, uint64_t above, double target)
+template <int THREADS, typename F> __device__ __forceinline__ void first_reaching(RowShared<THREADS>& sh, const F& f, uint64_t above, double target)
 {
-    constexpr int PER = kBins / THREADS, WAVES = THREADS / 64;
+    constexpr int PER = RowShared<THREADS>::BINS / THREADS, WAVES = THREADS / 64;
     const int t = threadIdx.x;
     uint64_t v[PER], mine = 0;
 #pragma unroll
@@ -240,81 +286,230 @@ template <int THREADS, typename F> __device__ __forceinline__ void first_reachin
     __syncthreads();
 }
 
-// The entries of the row that `want` takes into the list, in any order; false if they do not fit.
-template <typename ROW, typename F> __device__ __forceinline__ bool gather(RowShared& sh, const ROW& row, const F& want)
+// The entries that `want` takes into a list, in any order, their indices shifted by `offset`; *count goes on beyond LIST where they do not fit.
+template <int LIST, typename ROW, typename F> __device__ __forceinline__ void gather(uint64_t* list, uint32_t* count, const ROW& row, int offset, const F& want)
 {
-    __syncthreads();
-    if (threadIdx.x == 0) sh.count = 0;
-    __syncthreads();
-    row.each([&](int first, const typename ROW::vec& v) {
+    row.template each<4>([&](int first, const typename ROW::vec& v) {
         uint32_t hits = 0;
 #pragma unroll
         for (int e = 0; e < ROW::E; ++e) hits |= first + e < row.n && want(static_cast<float>(v[e])) ? 1u << e : 0u;
         if (hits) {   // rare
-            uint32_t at = atomicAdd(&sh.count, static_cast<uint32_t>(__popc(hits)));
+            uint32_t at = atomicAdd(count, static_cast<uint32_t>(__popc(hits)));
 #pragma unroll
             for (int e = 0; e < ROW::E; ++e)
                 if (hits >> e & 1) {
-                    if (at < kList) sh.list[at] = entry_of(static_cast<float>(v[e]), first + e);
+                    if (at < LIST) list[at] = entry_of(static_cast<float>(v[e]), offset + first + e);
                     ++at;
                 }
         }
     });
-    __syncthreads();
-    return sh.count <= kList;
 }
 
-// list[0 .. count) into bins[0 .. count), descending.  Up to 256 entries each finds its place by counting
-// the larger ones; more go through a bitonic network.
-template <int THREADS> __device__ __forceinline__ void sort_list(RowShared& sh, int count)
+// sh.list[0 .. count) into sh.sorted[0 .. count), descending.  Up to 256 entries each finds its place by counting the larger ones; more go through a
+// bitonic network.
+template <int THREADS> __device__ __forceinline__ void sort_list(RowShared<THREADS>& sh, int count)
 {
     const int t = threadIdx.x;
+    __syncthreads();
     if (count <= 256) {
+        if (t < 8 && count + t < 264) sh.list[count + t] = 0;   // (LIST is 512 or more)
+        __syncthreads();
         if (t < count) {
             const uint64_t e = sh.list[t];
             int rank = 0;
-            for (int j = 0; j < count; ++j) rank += sh.list[j] > e;
-            sh.bins[rank] = e;
+#pragma unroll 4
+            for (int j = 0; j < count; j += 2) {
+                const ulonglong2 o = *reinterpret_cast<const ulonglong2*>(&sh.list[j]);
+                rank += (o.x > e) + (o.y > e);
+            }
+            sh.sorted[rank] = e;
         }
         __syncthreads();
         return;
     }
-    int size = 512;
+    int size = 512;   // (at most LIST)
     while (size < count) size <<= 1;
-    for (int j = t; j < size; j += THREADS) sh.bins[j] = j < count ? sh.list[j] : 0;   // (no entry is 0: that is a NaN's key)
+    for (int j = t; j < size; j += THREADS) sh.sorted[j] = j < count ? sh.list[j] : 0;   // (no entry is 0: that is a NaN's key)
     for (int width = 2; width <= size; width <<= 1)
         for (int d = width >> 1; d; d >>= 1) {
             __syncthreads();
             for (int q = t; q < size / 2; q += THREADS) {
                 const int lo = (q & ~(d - 1)) * 2 + (q & (d - 1)), hi = lo + d;
-                const uint64_t x = sh.bins[lo], y = sh.bins[hi];
-                if ((x < y) == ((lo & width) == 0)) { sh.bins[lo] = y; sh.bins[hi] = x; }
+                const uint64_t x = sh.sorted[lo], y = sh.sorted[hi];
+                if ((x < y) == ((lo & width) == 0)) { sh.sorted[lo] = y; sh.sorted[hi] = x; }
             }
         }
     __syncthreads();
 }
 
-// The last entry that a filter keeps, in the key's digits: by_mass the first at which the mass reaches `target`, else the first at which the count does.
-// For rows whose equal scores overflow the list.
-template <int THREADS, typename ROW> __device__ __forceinline__ uint64_t last_by_digits(RowShared& sh, const ROW& row, const Weights& w, bool by_mass, double target)
+// What is known of a row once its largest and smallest score are.
+enum class Way { kRefused, kGreedy, kPlain, kShortList, kRange, kDigits };
+struct RowState {
+    Weights w;
+    float m, lo, per;   // scores in (lo, m] have mass; parts of that range per unit of score
+    Way way;
+    // (rounding is monotone)
+    template <int BINS> __device__ __forceinline__ int bin(float x) const { return min(static_cast<int>((m - x) * per), BINS - 1); }
+};
+template <int BINS> __device__ inline RowState row_state(const RowSettings& s, float hi, float low, bool nan)
 {
+    RowState st;
+    st.m = uniform(hi);
+    st.w = make_weights(st.m, s.t);
+    // entries below m - 28.5 T round to 0 units: whether a filter keeps them shows in nothing
+    st.lo = uniform(fmaxf(low, static_cast<float>(fmax(static_cast<double>(hi) - 28.5 * s.t, -0x1.fffffep127)) - 2e-7f * fabsf(hi)));
+    st.per = uniform(fminf(static_cast<float>(BINS) / (st.m - st.lo), 0x1.fffffep127f));
+    const bool flat = !(st.lo < st.m) || st.m - st.lo == INFINITY;   // no range to divide
+    st.way = s.bad || nan || st.m == -INFINITY ? Way::kRefused : s.greedy ? Way::kGreedy : s.k && s.k <= kListK ? Way::kShortList
+           : !s.k && !(s.p < 1.0) ? Way::kPlain : flat ? Way::kDigits : Way::kRange;
+    return st;
+}
+
+// Largest and smallest score and NaN of the stretch to every thread; the maxima of `groups` (a power of two, 4 to 256) groups of threads into group[].
+template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(RowShared<THREADS>& sh, const ROW& row, float* hi_out, float* low_out, uint32_t* group, int groups)
+{
+    float hi = -INFINITY, low = INFINITY;
+    bool nan = false;
+    row.template each<4>([&](int first, const typename ROW::vec& v) {
+#pragma unroll
+        for (int e = 0; e < ROW::E; ++e) {
+            const float x = static_cast<float>(v[e]);
+            nan |= x != x;
+            hi = fmaxf(hi, x);
+            low = first + e < row.n ? fminf(low, x) : low;
+        }
+    });
+    const int width = THREADS / groups;   // threads of a group
+    for (int d = 1; d < 64; d <<= 1) {
+        if (d == width && (row.lane & (d - 1)) == 0) group[threadIdx.x / d] = score_key(hi);
+        hi = fmaxf(hi, __shfl_xor(hi, d));
+        low = fminf(low, __shfl_xor(low, d));
+    }
+    if (row.lane == 0) { sh.part[row.wave] = score_key(hi); sh.part2[row.wave] = score_key(low); }
+    nan = __syncthreads_or(nan);
+    if (width >= 64 && static_cast<int>(threadIdx.x) < groups) {
+        uint64_t g = 0;
+        for (int q = 0; q < width / 64; ++q) g = max(g, sh.part[threadIdx.x * (width / 64) + q]);
+        group[threadIdx.x] = static_cast<uint32_t>(g);
+    }
+    for (int q = 0; q < ROW::WAVES; ++q) { hi = fmaxf(hi, key_score(static_cast<uint32_t>(sh.part[q]))); low = fminf(low, key_score(static_cast<uint32_t>(sh.part2[q]))); }
+    *hi_out = hi;
+    *low_out = low;
+    __syncthreads();
+    return nan;
+}
+
+// The k-th largest of sh.group[0 .. n) (of equals the k-th by number).
+template <int THREADS> __device__ __forceinline__ float kth_group(RowShared<THREADS>& sh, int n, int k)
+{
+    __syncthreads();
+    for (int t = threadIdx.x; t < n; t += THREADS) {
+        const uint32_t g = sh.group[t];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; j += 4) {   // (n is a multiple of 4)
+            const uint4 o = *reinterpret_cast<const uint4*>(&sh.group[j]);
+            rank += (o.x > g) + (o.y > g) + (o.z > g) + (o.w > g);
+            rank += ((o.x == g) & (j < t)) + ((o.y == g) & (j + 1 < t)) + ((o.z == g) & (j + 2 < t)) + ((o.w == g) & (j + 3 < t));
+        }
+        if (rank == k - 1) sh.bound = g;
+    }
+    __syncthreads();
+    return key_score(static_cast<uint32_t>(sh.bound));
+}
+
+// A row whose kept entries are all among the `count` of sh.list, the first s.k of which top-k keeps.
+template <int THREADS> __device__ __forceinline__ void draw_from_list(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r, const RowSettings& s, const Weights& w, int count)
+{
+    constexpr int WAVES = THREADS / 64;
+    const int t = threadIdx.x, wave = t >> 6;
+    sort_list<THREADS>(sh, count);
+    count = min(count, s.k);
+    // thread j has entry j of the order
+    const uint64_t e = t < count ? sh.sorted[t] : 0;
+    const double raw = t < count ? w.raw(entry_score(e)) : 0.0;
+    const uint64_t mine = Weights::whole_units(rint(raw));
+    uint64_t upto = wave_scan(mine);
+    if ((t & 63) == 63) sh.part[wave] = upto;
+    __syncthreads();
+    uint64_t mass = 0;
+    for (int q = 0; q < WAVES; ++q) { upto += q < wave ? sh.part[q] : 0; mass += sh.part[q]; }
+    const bool keep = t < count && (t == 0 || static_cast<double>(upto - mine) < s.p * static_cast<double>(mass) || s.p >= 1.0) && raw >= s.min_p * kUnits;
+    const uint64_t total = block_sum<WAVES>(sh.part, keep ? mine : 0);
+    if (t < kListK) { sh.list[t] = keep ? e : 0; sh.mass[t] = keep ? mine : 0; }
+    __syncthreads();
+    if (keep) {
+        const uint64_t target = static_cast<uint64_t>(s.u * static_cast<double>(total));
+        uint64_t before = 0;   // kept mass of lower indices
+#pragma unroll 8
+        for (int j = 0; j < count; ++j) before += static_cast<uint32_t>(sh.list[j]) > static_cast<uint32_t>(e) ? sh.mass[j] : 0;   // (a lower index has a larger complement)
+        if (before <= target && target < before + mine) answer(a, r, entry_index(e), log_probability(entry_score(e), w, s.t, total));
+    }
+}
+
+// The histogram of the stretch's scores: mass, entries, or both.
+template <int THREADS, typename ROW> __device__ __forceinline__ void fill_histogram(RowShared<THREADS>& sh, const ROW& row, const RowState& st, bool masses, bool entries)
+{
+    for (int b = threadIdx.x; b < RowShared<THREADS>::BINS; b += THREADS) { sh.mass[b] = 0; sh.entries[b] = 0; }
+    __syncthreads();
+    row.template each<1>([&](int, const typename ROW::vec& v) {
+        uint64_t u[ROW::E];
+        if (!ROW::any(v, st.lo)) return;
+        if (masses)
+#pragma unroll
+        for (int e = 0; e < ROW::E; ++e) {
+            u[e] = st.w.units(static_cast<float>(v[e]));
+            asm("" : "+v"(u[e]));   // here and not behind the test below: the exponentials of several scores overlap
+        }
+#pragma unroll
+        for (int e = 0; e < ROW::E; ++e) {
+            const float x = static_cast<float>(v[e]);
+            if (x >= st.lo) {
+                const int b = st.template bin<RowShared<THREADS>::BINS>(x);
+                if (masses) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]), static_cast<unsigned long long>(u[e]));
+                if (entries) atomicAdd(&sh.entries[b], 1u);
+            }
+        }
+    });
+    __syncthreads();
+}
+
+// The entry in sh.sorted[0 .. count) at which the count (or mass) reaches target, given what lies above the list; 0 if none does.  *mass: of the list's entries down to it.
+template <int THREADS>
+__device__ __forceinline__ uint64_t last_in_list(RowShared<THREADS>& sh, const Weights& w, int count, bool by_mass, uint64_t above, double target, uint64_t* mass)
+{
+    sort_list<THREADS>(sh, count);
+    first_reaching<THREADS>(sh, [&](int j) -> uint64_t { return j >= count ? 0 : by_mass ? w.units(entry_score(sh.sorted[j])) : 1; }, above, target);
+    const int b = sh.pick;
+    uint64_t sum = 0;
+    for (int j = threadIdx.x; j < count; j += THREADS) sum += b >= 0 && j <= b ? w.units(entry_score(sh.sorted[j])) : 0;
+    *mass = block_sum<THREADS / 64>(sh.part, sum);
+    return b < 0 ? 0 : sh.sorted[b];
+}
+
+// The last entry that a filter keeps, in the key's digits: by_mass the first at which the mass reaches `target`, else the first at which the count does.
+template <int THREADS, typename ROW> __device__ __forceinline__ uint64_t last_by_digits(RowShared<THREADS>& sh, const ROW& row, const Weights& w, bool by_mass, double target)
+{
+    constexpr int BINS = RowShared<THREADS>::BINS, BITS = BINS == 2048 ? 11 : 9;
+    static_assert(BINS == 1 << BITS, "a digit's values have a bin each");
     uint32_t prefix = 0;
     uint64_t above = 0;
 #pragma unroll 1
-    for (int round = 0; round < 3; ++round) {
-        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+    for (int shift = 32; shift > 0;) {
+        const int bits = min(shift, BITS), had = shift;
+        shift -= bits;
         __syncthreads();
-        for (int b = threadIdx.x; b < kBins; b += THREADS) sh.bins[b] = 0;
+        for (int b = threadIdx.x; b < BINS; b += THREADS) sh.mass[b] = 0;
         __syncthreads();
         row.each_score([&](float x, int index) {
             const uint32_t key = score_key(x);
-            if (index >= row.n || (round > 0 && key >> (shift + bits) != prefix)) return;
+            if (index >= row.n || (had < 32 && key >> had != prefix)) return;
             const uint64_t v = by_mass ? w.units(x) : 1;
-            if (v) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[(key >> shift) & ((1u << bits) - 1)]), static_cast<unsigned long long>(v));
+            if (v) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[(key >> shift) & ((1u << bits) - 1)]), static_cast<unsigned long long>(v));
         });
         __syncthreads();
-        first_reaching<THREADS>(sh, [&](int j) { return sh.bins[kBins - 1 - j]; }, above, target);
-        prefix = prefix << bits | static_cast<uint32_t>(kBins - 1 - sh.pick);
+        first_reaching<THREADS>(sh, [&](int j) { return sh.mass[BINS - 1 - j]; }, above, target);
+        prefix = prefix << bits | static_cast<uint32_t>(BINS - 1 - sh.pick);
         above = sh.pick_sum;
     }
     // among the entries of that score the r-th in index order
@@ -337,7 +532,7 @@ template <int THREADS, typename ROW> __device__ __forceinline__ uint64_t last_by
         if (owner < 0) left -= c;
     }
     if (row.wave == owner) {
-        row.each([&](int first, const typename ROW::vec& v8) {
+        row.template each<1>([&](int first, const typename ROW::vec& v8) {
             uint64_t c = 0;
 #pragma unroll
             for (int e = 0; e < ROW::E; ++e) c += first + e < row.n && score_key(static_cast<float>(v8[e])) == prefix;
@@ -347,8 +542,7 @@ template <int THREADS, typename ROW> __device__ __forceinline__ uint64_t last_by
                 int64_t need = left - before;
 #pragma unroll
                 for (int e = 0; e < ROW::E; ++e)
-                    if (first + e < row.n && score_key(static_cast<float>(v8[e])) == prefix && --need == 0)
-                        sh.bound = entry_of(static_cast<float>(v8[e]), first + e);
+                    if (first + e < row.n && score_key(static_cast<float>(v8[e])) == prefix && --need == 0) sh.bound = entry_of(static_cast<float>(v8[e]), first + e);
             }
             left = left > all ? left - all : 0;
         });
@@ -357,219 +551,179 @@ template <int THREADS, typename ROW> __device__ __forceinline__ uint64_t last_by
     return sh.bound;
 }
 
-// The same through the histogram over [lo, m], into *last, which stays as it is if the crossing is not above lo.  What lies below lo is known not to matter: it
-// has no mass, or lies beyond the crossing.  false if one part of the range overflows the list.
-template <int THREADS, typename ROW>
-__device__ __forceinline__ bool last_by_range(RowShared& sh, const ROW& row, const Weights& w, float m, float lo, bool by_mass, double target, uint64_t* last)
-{
-    const float per = fminf(static_cast<float>(kBins) / (m - lo), 0x1.fffffep127f);
-    auto bin = [&](float x) { return min(static_cast<int>((m - x) * per), kBins - 1); };   // (rounding is monotone)
-    __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += THREADS) sh.bins[b] = 0;
-    __syncthreads();
-    row.each_score([&](float x, int) {
-        if (x < lo) return;
-        const uint64_t v = by_mass ? w.units(x) : 1;
-        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.bins[bin(x)]), static_cast<unsigned long long>(v));
-    });
-    __syncthreads();
-    uint64_t above = 0;
-    int count = kBins;
-#pragma unroll 1
-    for (int pass = 0; pass < 2; ++pass) {   // the part of the range, then the entry in the sorted list
-        first_reaching<THREADS>(sh, [&](int j) -> uint64_t { return pass == 0 ? sh.bins[j] : j >= count ? 0 : by_mass ? w.units(entry_score(sh.bins[j])) : 1; }, above, target);
-        const int b = sh.pick;
-        if (b < 0) return true;
-        if (pass == 1) {
-            *last = sh.bins[b];
-            return true;
-        }
-        above = sh.pick_sum;
-        if (!gather(sh, row, [&](float x) { return x >= lo && bin(x) == b; })) return false;
-        count = static_cast<int>(sh.count);
-        sort_list<THREADS>(sh, count);
+// What of a stretch is kept: entries down to `last` (0: all) whose weight min-p allows; `offset` is the index of the stretch's first score.
+struct Kept {
+    float score;
+    int index;
+    double min_raw;
+    __device__ Kept(uint64_t last, int offset, double min_p) : score(last ? entry_score(last) : -INFINITY), index(last ? entry_index(last) - offset : 0x7FFFFFFF), min_raw(min_p * kUnits) {}
+    __device__ __forceinline__ double operator()(const Weights& w, float x, int i) const
+    {
+        const double raw = w.raw(x);
+        const bool in = (x > score) | ((x == score) & (i <= index));
+        return (in & (raw >= min_raw)) ? rint(raw) : 0.0;   // (no branches: the exponentials of several scores overlap)
     }
-    return true;
+};
+
+// The draw from a stretch.  total: all kept mass of the row and target what is left of u's share of it where the stretch begins; where total is 0, the stretch is the whole row and both are found here.
+template <int THREADS, typename ROW>
+__device__ __forceinline__ void draw(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r, const ROW& row, int offset, const RowSettings& s, const Weights& w, uint64_t last, uint64_t total,
+                                     uint64_t target)
+{
+    constexpr int WAVES = THREADS / 64, E = ROW::E;
+    const Kept kept(last, offset, s.min_p);
+    const int t = threadIdx.x, per = (row.trips + 3) / 4;
+    uint64_t sums[4] = {0, 0, 0, 0};   // of four groups of this lane's trips
+    {
+        double sum = 0.0;
+        int left = per, group = 0;
+        auto close = [&] {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) sums[q] = q == group ? Weights::whole_units(sum) : sums[q];
+            sum = 0.0;
+            left = per;
+            ++group;
+        };
+        row.template each<1>([&](int first, const typename ROW::vec& v) {
+            if (ROW::any(v, kept.score)) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum += kept(w, static_cast<float>(v[e]), first + e);
+            }
+            if (--left == 0) close();
+        });
+        if (left < per) close();
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sums[q] = wave_sum(sums[q]);
+    __syncthreads();
+    if (row.lane < 4) sh.mass[row.wave * 4 + row.lane] = row.lane == 0 ? sums[0] : row.lane == 1 ? sums[1] : row.lane == 2 ? sums[2] : sums[3];
+    __syncthreads();
+    if (total == 0) {
+        for (int q = 0; q < 4 * WAVES; ++q) total += sh.mass[q];
+        target = static_cast<uint64_t>(s.u * static_cast<double>(total));
+    }
+    int owner = -1;
+    for (int q = 0; q < 4 * WAVES; ++q) {
+        if (owner < 0 && target < sh.mass[q]) owner = q;
+        if (owner < 0) target -= sh.mass[q];
+    }
+    // the stretch of that group, shared out among all threads
+    const int begin = ((owner >> 2) * row.trips + (owner & 3) * per) * 64 * E, end = min(row.n, ((owner >> 2) * row.trips + min(((owner & 3) + 1) * per, row.trips)) * 64 * E);
+    const int each = (end - begin + THREADS - 1) / THREADS, from = begin + t * each, to = min(end, from + each);
+    double sum = 0.0;
+    for (int i = from; i < to; ++i) sum += kept(w, static_cast<float>(row.x[i]), i);
+    const uint64_t own = Weights::whole_units(sum);
+    uint64_t upto = wave_scan(own);
+    if (row.lane == 63) sh.part[row.wave] = upto;
+    __syncthreads();
+    for (int q = 0; q < WAVES; ++q) upto += q < row.wave ? sh.part[q] : 0;
+    if (target < upto - own || target >= upto) return;
+    uint64_t at = upto - own;
+    for (int i = from; i < to; ++i) {
+        const float x = static_cast<float>(row.x[i]);
+        at += Weights::whole_units(kept(w, x, i));
+        if (target < at) return answer(a, r, offset + i, log_probability(x, w, s.t, total));
+    }
+}
+
+// The lowest index of the row's maximum in the stretch, or 2^31 - 1.
+template <int THREADS, typename ROW> __device__ __forceinline__ int first_of(RowShared<THREADS>& sh, const ROW& row, float m)
+{
+    int first = 0x7FFFFFFF;
+    row.template each<4>([&](int at, const typename ROW::vec& v) {
+#pragma unroll
+        for (int e = 0; e < ROW::E; ++e) first = static_cast<float>(v[e]) == m ? min(first, at + e) : first;
+    });
+    for (int d = 32; d; d >>= 1) first = min(first, __shfl_xor(first, d));
+    __syncthreads();
+    if (row.lane == 0) sh.part[row.wave] = static_cast<uint64_t>(first);
+    __syncthreads();
+    for (int q = 0; q < ROW::WAVES; ++q) first = min(first, static_cast<int>(sh.part[q]));
+    return first;
+}
+
+// ---- a row by one workgroup -----------------------------------------------------------------------------------------------
+template <typename T, int THREADS> __device__ __forceinline__ void whole_row(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r)
+{
+    typedef Row<T, THREADS> ROW;
+    const ROW row(a, r, 0, a.n);
+    const RowSettings s = row_settings(a, r);
+    float hi, low;
+    const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, 256);
+    const RowState st = row_state<RowShared<THREADS>::BINS>(s, hi, low, nan);
+    if (st.way == Way::kRefused) {
+        if (threadIdx.x == 0) answer(a, r, -1, not_a_number());
+        return;
+    }
+    if (st.way == Way::kGreedy) {
+        const int first = first_of(sh, row, st.m);
+        if (threadIdx.x == 0) answer(a, r, first, 0.f);
+        return;
+    }
+    if (threadIdx.x == 0) sh.count = 0;
+    if (st.way == Way::kShortList) {
+        const float bound = kth_group<THREADS>(sh, 256, s.k);
+        gather<RowShared<THREADS>::LIST>(sh.list, &sh.count, row, 0, [&](float x) { return x >= bound && x > -INFINITY; });   // (fewer than k finite scores: bound is -infinity)
+        __syncthreads();
+        if (sh.count <= RowShared<THREADS>::LIST) return draw_from_list<THREADS>(sh, a, r, s, st.w, static_cast<int>(sh.count));
+    }
+    uint64_t last = 0;
+    bool by_digits = st.way == Way::kDigits || st.way == Way::kShortList;
+    if (st.way == Way::kRange) {
+        fill_histogram<THREADS>(sh, row, st, s.p < 1.0, s.k > 0);
+        uint64_t kept_mass = 0;   // of what top-k leaves
+#pragma unroll 1
+        for (int filter = s.k ? 0 : 1; filter < (s.p < 1.0 ? 2 : 1) && !by_digits; ++filter) {
+            const bool by_mass = filter == 1;
+            if (!s.k || (by_mass && kept_mass == 0)) {   // all of it
+                uint64_t sum = 0;
+                for (int b = threadIdx.x; b < RowShared<THREADS>::BINS; b += THREADS) sum += sh.mass[b];
+                kept_mass = block_sum<THREADS / 64>(sh.part, sum);
+            }
+            const double target = by_mass ? s.p * static_cast<double>(kept_mass) : s.k;
+            first_reaching<THREADS>(sh, [&](int j) -> uint64_t { return by_mass ? sh.mass[j] : sh.entries[j]; }, 0, target);
+            const int b = sh.pick;
+            const uint64_t above = sh.pick_sum;
+            if (b < 0) continue;   // fewer than k have mass: all of them are kept
+            uint64_t sum = 0;
+            for (int j = threadIdx.x; j < b; j += THREADS) sum += sh.mass[j];
+            sum = block_sum<THREADS / 64>(sh.part, sum);
+            if (threadIdx.x == 0) sh.count = 0;
+            __syncthreads();
+            gather<RowShared<THREADS>::LIST>(sh.list, &sh.count, row, 0, [&](float x) { return x >= st.lo && st.template bin<RowShared<THREADS>::BINS>(x) == b; });
+            __syncthreads();
+            if (sh.count > RowShared<THREADS>::LIST) { by_digits = true; break; }
+            uint64_t mass;
+            last = last_in_list<THREADS>(sh, st.w, static_cast<int>(sh.count), by_mass, above, target, &mass);
+            kept_mass = sum + mass;
+        }
+    }
+    if (by_digits) {
+        last = 0;
+        uint64_t floor = st.m == INFINITY ? static_cast<uint64_t>(score_key(INFINITY)) << 32 : 0;   // beside +infinity nothing has mass
+#pragma unroll 1
+        for (int filter = 0; filter < 2; ++filter) {
+            if (filter == 0 ? !s.k : !(s.p < 1.0)) continue;
+            double target = s.k;
+            if (filter == 1) {
+                double sum = 0.0;
+                row.each_score([&](float x, int index) {
+                    if (x > -INFINITY && entry_of(x, index) >= max(last, floor)) sum += st.w.whole(x);
+                });
+                target = s.p * static_cast<double>(block_sum<THREADS / 64>(sh.part, Weights::whole_units(sum)));
+            }
+            last = last_by_digits<THREADS>(sh, row, st.w, filter == 1, target);
+        }
+        last = max(last, floor);
+    }
+    draw<THREADS>(sh, a, r, row, 0, s, st.w, last, 0, 0);
 }
 
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a)
 {
-    typedef Row<T, THREADS> ROW;
-    constexpr int WAVES = THREADS / 64, E = ROW::E;
-    __shared__ RowShared sh;
-    const int64_t r = blockIdx.x;
-    const int t = threadIdx.x;
-    const ROW row(a, r);
-    const RowSettings s = row_settings(a, r);
-    // largest and smallest score, and whether there is a NaN
-    float hi = -INFINITY, low = INFINITY;
-    bool nan = false;
-    row.each([&](int, const typename ROW::vec& v) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float x = static_cast<float>(v[e]);
-            nan |= x != x;
-            hi = fmaxf(hi, x);
-            low = fminf(low, x);
-        }
-    });
-    {   // 256 groups of threads
-        float g = hi;
-        if constexpr (THREADS == 1024) { g = fmaxf(g, __shfl_xor(g, 1)); g = fmaxf(g, __shfl_xor(g, 2)); }
-        if (THREADS == 256 || (t & 3) == 0) sh.group[THREADS == 256 ? t : t >> 2] = score_key(g);
-        for (int d = 32; d; d >>= 1) { hi = fmaxf(hi, __shfl_xor(hi, d)); low = fminf(low, __shfl_xor(low, d)); }
-        if (row.lane == 0) { sh.part[row.wave] = score_key(hi); sh.part2[row.wave] = score_key(low); }
-        nan = __syncthreads_or(nan);
-        for (int q = 0; q < WAVES; ++q) { hi = fmaxf(hi, key_score(static_cast<uint32_t>(sh.part[q]))); low = fminf(low, key_score(static_cast<uint32_t>(sh.part2[q]))); }
-    }
-    const float m = hi;
-    if (s.bad || nan || m == -INFINITY) {
-        if (t == 0) answer(a, r, -1, not_a_number());
-        return;
-    }
-    if (s.greedy) {
-        int first = 0x7FFFFFFF;
-        row.each_score([&](float x, int index) { if (x == m && index < first) first = index; });
-        for (int d = 32; d; d >>= 1) first = min(first, __shfl_xor(first, d));
-        __syncthreads();
-        if (row.lane == 0) sh.part[row.wave] = static_cast<uint64_t>(first);
-        __syncthreads();
-        for (int q = 0; q < WAVES; ++q) first = min(first, static_cast<int>(sh.part[q]));
-        if (t == 0) answer(a, r, first, 0.f);
-        return;
-    }
-    const Weights w = make_weights(m, s.t);
-    const double min_raw = s.min_p * kUnits;
-    // ---- top-k by the list
-    if (s.k && s.k <= kListK) {
-        if (t < kGroups) {   // the k-th largest of the groups' maxima (the k-th of equals by number)
-            const uint32_t g = sh.group[t];
-            int rank = 0;
-            for (int j = 0; j < kGroups; ++j) rank += sh.group[j] > g || (sh.group[j] == g && j < t);
-            if (rank == s.k - 1) sh.bound = g;
-        }
-        __syncthreads();
-        const float bound = key_score(static_cast<uint32_t>(sh.bound));
-        if (gather(sh, row, [&](float x) { return x >= bound && x > -INFINITY; })) {   // (fewer than k finite scores: bound is -infinity)
-            int count = static_cast<int>(sh.count);
-            sort_list<THREADS>(sh, count);
-            count = min(count, s.k);
-            // thread j has entry j of the order
-            const uint64_t e = t < count ? sh.bins[t] : 0;
-            const double raw = t < count ? w.raw(entry_score(e)) : 0.0;
-            const uint64_t mine = static_cast<uint64_t>(rint(raw));
-            uint64_t upto = wave_scan(mine);
-            __syncthreads();
-            if (row.lane == 63) sh.part[row.wave] = upto;
-            __syncthreads();
-            uint64_t mass = 0;
-            for (int q = 0; q < WAVES; ++q) { upto += q < row.wave ? sh.part[q] : 0; mass += sh.part[q]; }
-            const bool keep = t < count && (t == 0 || static_cast<double>(upto - mine) < s.p * static_cast<double>(mass) || s.p >= 1.0) && raw >= min_raw;
-            // back in index order: the kept ones lead the order, so entry j's place is the number of kept ones with a lower index
-            const uint64_t total = block_sum<WAVES>(sh.part, keep ? mine : 0);
-            if (t < kListK) sh.list[t] = keep ? e : 0;
-            if (t < kListK) sh.bins[kListK + t] = keep ? mine : 0;
-            __syncthreads();
-            if (keep) {
-                const uint64_t target = static_cast<uint64_t>(s.u * static_cast<double>(total));
-                uint64_t before = 0;
-                for (int j = 0; j < count; ++j) before += static_cast<uint32_t>(sh.list[j]) > static_cast<uint32_t>(e) ? sh.bins[kListK + j] : 0;   // (a lower index has a larger complement)
-                if (before <= target && target < before + mine) answer(a, r, entry_index(e), log_probability(entry_score(e), w, s.t, total));
-            }
-            return;
-        }
-    }
-    // ---- the last entry of the kept prefix
-    uint64_t last = 0;
-    // entries below m - 28.5 T round to 0 units: whether a filter keeps them shows in nothing
-    const float no_mass = fmaxf(low, static_cast<float>(fmax(static_cast<double>(m) - 28.5 * s.t, -0x1.fffffep127)) - 2e-7f * fabsf(m));
-    const bool flat = w.inf || !(no_mass < m) || m - no_mass == INFINITY;   // no range to divide
-#pragma unroll 1
-    for (int filter = 0; filter < 2; ++filter) {   // top-k by the count, then top-p by the mass of what that left
-        const bool by_mass = filter == 1;
-        if (by_mass ? !(s.p < 1.0) : !s.k) continue;
-        double target = s.k;
-        float lo = no_mass;
-        if (by_mass) {
-            double sum = 0.0;
-            row.each([&](int first, const typename ROW::vec& v) {
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float x = static_cast<float>(v[e]);
-                    sum += entry_of(x, first + e) >= last ? w.whole(x) : 0.0;
-                }
-            });
-            const double mass = static_cast<double>(block_sum<WAVES>(sh.part, static_cast<uint64_t>(sum)));
-            target = s.p * mass;
-            // an entry is kept only if the mass from it on exceeds (1 - p) mass, and at most n entries no heavier than it make that up
-            const double least = (1.0 - s.p) * mass / kUnits / (s.k ? s.k : a.n) * (1.0 - 1e-6);
-            lo = fmaxf(lo, static_cast<float>(static_cast<double>(m) + s.t * log(least) * (1.0 + 1e-6)) - 1e-6f * fabsf(m));
-        }
-        bool by_digits = flat || !(lo < m);
-        if (!by_digits) by_digits = !last_by_range<THREADS>(sh, row, w, m, lo, by_mass, target, &last);
-        if (by_digits) last = last_by_digits<THREADS>(sh, row, w, by_mass, target);
-    }
-    // ---- the draw: per lane the kept mass of four groups of trips
-    auto kept = [&](float x, int index) {
-        if (x == -INFINITY || entry_of(x, index) < last) return 0.0;
-        const double raw = w.raw(x);
-        return raw >= min_raw ? rint(raw) : 0.0;
-    };
-    const int per = (row.trips + 3) / 4;
-    uint64_t sums[4] = {0, 0, 0, 0};
-#pragma unroll 1
-    for (int g = 0; g < 4; ++g) {
-        double sum = 0.0;
-        row.each(g * per, min((g + 1) * per, row.trips), [&](int first, const typename ROW::vec& v) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) sum += kept(static_cast<float>(v[e]), first + e);
-        });
-#pragma unroll
-        for (int q = 0; q < 4; ++q) sums[q] = q == g ? static_cast<uint64_t>(sum) : sums[q];
-    }
-    const uint64_t mine = wave_sum(sums[0] + sums[1] + sums[2] + sums[3]);
-    __syncthreads();
-    if (row.lane == 0) sh.part[row.wave] = mine;
-    __syncthreads();
-    uint64_t total = 0;
-    for (int q = 0; q < WAVES; ++q) total += sh.part[q];
-    uint64_t target = static_cast<uint64_t>(s.u * static_cast<double>(total));
-    int owner = -1;
-    for (int q = 0; q < WAVES; ++q) {
-        if (owner < 0 && target < sh.part[q]) owner = q;
-        if (owner < 0) target -= sh.part[q];
-    }
-    if (row.wave != owner) return;
-    int group = -1;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const uint64_t g = wave_sum(sums[q]);
-        if (group < 0 && target < g) group = q;
-        if (group < 0) target -= g;
-    }
-    bool found = false;
-    row.each(group * per, min((group + 1) * per, row.trips), [&](int first, const typename ROW::vec& v) {
-        if (found) return;
-        double sum = 0.0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum += kept(static_cast<float>(v[e]), first + e);
-        const uint64_t own = static_cast<uint64_t>(sum), upto = wave_scan(own), all = __shfl(upto, 63);
-        if (target >= all) { target -= all; return; }
-        found = true;
-        if (target < upto - own || target >= upto) return;
-        uint64_t at = upto - own;
-        bool done = false;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float x = static_cast<float>(v[e]);
-            at += static_cast<uint64_t>(kept(x, first + e));
-            if (!done && target < at) {
-                done = true;
-                answer(a, r, first + e, log_probability(x, w, s.t, total));
-            }
-        }
-    });
+    __shared__ RowShared<THREADS> sh;
+    whole_row<T, THREADS>(sh, a, blockIdx.x);
 }
 
 template <typename T> static void launch_policy(const PolicyArgs& a, int64_t rows, hipStream_t st)
