@@ -399,20 +399,23 @@ template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(Ro
     return nan;
 }
 
-// The k-th largest of sh.group[0 .. n) (of equals the k-th by number).
+// How many groups: enough that the entries above the k-th largest maximum are few more than k, few enough to rank.
+__device__ __host__ inline int groups_for(int k) { return k <= 24 ? 64 : k <= 64 ? 128 : 256; }
+
+// The k-th largest of sh.group[0 .. n).
 template <int THREADS> __device__ __forceinline__ float kth_group(RowShared<THREADS>& sh, int n, int k)
 {
     __syncthreads();
     for (int t = threadIdx.x; t < n; t += THREADS) {
         const uint32_t g = sh.group[t];
-        int rank = 0;
-#pragma unroll 8
+        int more = 0, as_many = 0;
+#pragma unroll 4
         for (int j = 0; j < n; j += 4) {   // (n is a multiple of 4)
             const uint4 o = *reinterpret_cast<const uint4*>(&sh.group[j]);
-            rank += (o.x > g) + (o.y > g) + (o.z > g) + (o.w > g);
-            rank += ((o.x == g) & (j < t)) + ((o.y == g) & (j + 1 < t)) + ((o.z == g) & (j + 2 < t)) + ((o.w == g) & (j + 3 < t));
+            more += (o.x > g) + (o.y > g) + (o.z > g) + (o.w > g);
+            as_many += (o.x >= g) + (o.y >= g) + (o.z >= g) + (o.w >= g);
         }
-        if (rank == k - 1) sh.bound = g;
+        if (more < k && k <= as_many) sh.bound = g;   // (equals write the same)
     }
     __syncthreads();
     return key_score(static_cast<uint32_t>(sh.bound));
@@ -649,7 +652,8 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
     const ROW row(a, r, 0, a.n);
     const RowSettings s = row_settings(a, r);
     float hi, low;
-    const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, 256);
+    const int groups = groups_for(s.k);
+    const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, groups);
     const RowState st = row_state<RowShared<THREADS>::BINS>(s, hi, low, nan);
     if (st.way == Way::kRefused) {
         if (threadIdx.x == 0) answer(a, r, -1, not_a_number());
@@ -662,7 +666,7 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
     }
     if (threadIdx.x == 0) sh.count = 0;
     if (st.way == Way::kShortList) {
-        const float bound = kth_group<THREADS>(sh, 256, s.k);
+        const float bound = kth_group<THREADS>(sh, groups, s.k);
         gather<RowShared<THREADS>::LIST>(sh.list, &sh.count, row, 0, [&](float x) { return x >= bound && x > -INFINITY; });   // (fewer than k finite scores: bound is -infinity)
         __syncthreads();
         if (sh.count <= RowShared<THREADS>::LIST) return draw_from_list<THREADS>(sh, a, r, s, st.w, static_cast<int>(sh.count));
@@ -726,21 +730,243 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a)
     whole_row<T, THREADS>(sh, a, blockIdx.x);
 }
 
-template <typename T> static void launch_policy(const PolicyArgs& a, int64_t rows, hipStream_t st)
+// ---- few long rows: a row by several workgroups ------------------------------------------------------------------------------
+//
+// One compute unit takes 30 to 120 us for a row of 131072, so a few rows are shared out: `parts` workgroups per row, a launch for each point at which they have to
+// know of each other (no workgroup waits for another one), and in between a record per row in the caller's workspace.
+//   1  extremes, groups' maxima                     2  short list | histogram | kept mass of each part
+//   3  draw (short list, no filter) | entries of the part of the range that the last kept one lies in, kept mass above it        4  draw
+// A row that the list or the range cannot hold is done by one workgroup in the last launch.
+constexpr int kParts = 64, kPartThreads = 1024, kPartMin = 4096;
+typedef RowShared<kPartThreads> PartShared;
+
+struct SplitRow {
+    uint64_t mass[PartShared::BINS];
+    uint32_t entries[PartShared::BINS];
+    uint64_t list[2][PartShared::LIST];
+    uint64_t kept[kParts];
+    uint32_t hi[kParts], low[kParts], nan[kParts], first[kParts];
+    uint32_t group[kPolicyGroups];
+    uint32_t count[2];   // entries in the lists: the last kept one is among the second where both filters are on, top-k's border in the first
+};
+
+struct SplitPlan { int parts, len, groups; };   // len: scores of a part, groups per part
+static SplitPlan split_plan(int64_t rows, int64_t n)
+{
+    SplitPlan p{1, static_cast<int>(n), 0};
+    if (rows < 1 || rows > 64 || n < 4 * kPartMin) return p;
+    int64_t parts = n / kPartMin;
+    if (parts > 256 / rows) parts = 256 / rows;
+    if (parts > kParts) parts = kParts;
+    p.len = static_cast<int>(((n + parts - 1) / parts + 511) / 512 * 512);
+    p.parts = static_cast<int>((n + p.len - 1) / p.len);
+    p.groups = 4;
+    while (p.groups * p.parts < 256) p.groups *= 2;   // (256 to 511 in all)
+    return p;
+}
+
+template <typename T, int PHASE>
+__global__ __launch_bounds__(kPartThreads) void policy_split_kernel(PolicyArgs a, SplitPlan plan, SplitRow* records, int last_phase)
+{
+    constexpr int THREADS = kPartThreads, WAVES = THREADS / 64, BINS = PartShared::BINS, LIST = PartShared::LIST;
+    typedef Row<T, THREADS> ROW;
+    __shared__ PartShared sh;
+    const int64_t r = blockIdx.y;
+    const int part = blockIdx.x, t = threadIdx.x, from = part * plan.len;
+    SplitRow& rec = records[r];
+    const ROW row(a, r, from, min(plan.len, a.n - from));
+    const RowSettings s = row_settings(a, r);
+    if constexpr (PHASE == 1) {
+        float hi, low;
+        const bool nan = extremes<THREADS>(sh, row, &hi, &low, rec.group + part * plan.groups, plan.groups);
+        if (t == 0) { rec.hi[part] = score_key(hi); rec.low[part] = score_key(low); rec.nan[part] = nan; }
+        for (int b = part * THREADS + t; b < BINS; b += plan.parts * THREADS) { rec.mass[b] = 0; rec.entries[b] = 0; }
+        if (part == 0 && t < 2) rec.count[t] = 0;
+        return;
+    }
+    // every wavefront looks at all parts' extremes
+    uint32_t hi = 0, low = 0xFFFFFFFFu;
+    bool nan = false;
+    if (row.lane < plan.parts) { hi = rec.hi[row.lane]; low = rec.low[row.lane]; nan = rec.nan[row.lane] != 0; }
+    for (int d = 32; d; d >>= 1) { hi = max(hi, static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi), d))); low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), d))); }
+    nan = __any(nan);
+    const RowState st = row_state<BINS>(s, key_score(hi), key_score(low), nan);
+    const bool both = s.k && s.p < 1.0;
+    // the part that u's share of the kept mass falls into, given all parts' kept mass in sh.mass: its workgroup draws
+    auto draw_in_part = [&](uint64_t last) {
+        uint64_t total = 0;
+        for (int q = 0; q < plan.parts; ++q) total += sh.mass[q];
+        uint64_t target = static_cast<uint64_t>(s.u * static_cast<double>(total));
+        int owner = -1;
+        for (int q = 0; q < plan.parts; ++q) {
+            if (owner < 0 && target < sh.mass[q]) owner = q;
+            if (owner < 0) target -= sh.mass[q];
+        }
+        __syncthreads();
+        if (owner == part) draw<THREADS>(sh, a, r, row, from, s, st.w, last, total, target);
+    };
+    if constexpr (PHASE == 2) {
+        if (st.way == Way::kGreedy) {
+            const int first = first_of(sh, row, st.m);
+            if (t == 0) rec.first[part] = first == 0x7FFFFFFF ? 0x7FFFFFFFu : static_cast<uint32_t>(from + first);
+        } else if (st.way == Way::kShortList) {
+            const int groups = plan.parts * plan.groups;
+            for (int g = t; g < groups; g += THREADS) sh.group[g] = rec.group[g];
+            const float bound = kth_group<THREADS>(sh, groups, s.k);
+            gather<LIST>(rec.list[0], &rec.count[0], row, from, [&](float x) { return x >= bound && x > -INFINITY; });
+        } else if (st.way == Way::kRange) {
+            fill_histogram<THREADS>(sh, row, st, s.p < 1.0, s.k > 0);
+            for (int b = t; b < BINS; b += THREADS) {
+                if (sh.mass[b]) atomicAdd(reinterpret_cast<unsigned long long*>(&rec.mass[b]), static_cast<unsigned long long>(sh.mass[b]));
+                if (sh.entries[b]) atomicAdd(&rec.entries[b], sh.entries[b]);
+            }
+        } else if (st.way == Way::kPlain) {
+            const Kept kept(0, from, s.min_p);
+            double sum = 0.0;
+            row.each_score([&](float x, int index) { sum += kept(st.w, x, index); });
+            const uint64_t all = block_sum<WAVES>(sh.part, Weights::whole_units(sum));
+            if (t == 0) rec.kept[part] = all;
+        }
+        return;
+    }
+    // ---- rows that are answered here
+    if (PHASE == 3 && (st.way == Way::kRefused || st.way == Way::kGreedy)) {
+        if (part != 0 || t != 0) return;
+        uint32_t first = 0x7FFFFFFFu;
+        if (st.way == Way::kGreedy)
+            for (int q = 0; q < plan.parts; ++q) first = min(first, rec.first[q]);
+        st.way == Way::kGreedy ? answer(a, r, static_cast<int32_t>(first), 0.f) : answer(a, r, -1, not_a_number());
+        return;
+    }
+    if (PHASE == 3 && st.way == Way::kPlain) {
+        if (t < plan.parts) sh.mass[t] = rec.kept[t];
+        __syncthreads();
+        return draw_in_part(0);
+    }
+    auto fetch_list = [&](int which) {   // into sh.list; false if it overflowed
+        const uint32_t count = rec.count[which];
+        if (count > LIST) return false;
+        for (uint32_t j = t; j < count; j += THREADS) sh.list[j] = rec.list[which][j];
+        return true;
+    };
+    bool one_workgroup = st.way == Way::kDigits;
+    if (st.way == Way::kShortList) {
+        one_workgroup = rec.count[0] > LIST;
+        if (PHASE == 3 && !one_workgroup && part == 0) {
+            fetch_list(0);
+            draw_from_list<THREADS>(sh, a, r, s, st.w, static_cast<int>(rec.count[0]));
+        }
+    }
+    if (st.way == Way::kRange) {
+        auto border = [&](bool by_mass, double target, uint64_t* above) {   // the part of the range, or -1: all is kept
+            first_reaching<THREADS>(sh, [&](int j) -> uint64_t { return by_mass ? rec.mass[j] : rec.entries[j]; }, 0, target);
+            *above = sh.pick_sum;
+            return sh.pick;
+        };
+        auto mass_before = [&](int b) {   // of the parts of the range before b
+            uint64_t sum = 0;
+            for (int j = t; j < b; j += THREADS) sum += rec.mass[j];
+            return block_sum<WAVES>(sh.part, sum);
+        };
+        auto in_range = [&](float x, int b0, int b1) { return x >= st.lo && st.template bin<BINS>(x) >= b0 && st.template bin<BINS>(x) <= b1; };
+        uint64_t above, ignored;
+        int k_bin = -1, first = 0, second = -1;   // top-k's part of the range (-1: it keeps all); the parts first .. second of the last kept entry (none: all is kept)
+        uint64_t k_above = 0, k_mass = 0;
+        if (s.k) {
+            k_bin = border(false, s.k, &k_above);
+            k_mass = mass_before(k_bin < 0 ? BINS : k_bin);
+            first = second = k_bin;
+            if (k_bin < 0) first = 0;
+        } else {
+            first = second = border(true, s.p * static_cast<double>(mass_before(BINS)), &ignored);
+        }
+        if (both) {   // what top-k leaves of its part is not known before its list is: top-p's border between the extremes
+            const uint64_t most = k_mass + (k_bin < 0 ? 0 : rec.mass[k_bin]);
+            first = max(border(true, s.p * static_cast<double>(k_mass), &ignored), 0);
+            second = border(true, s.p * static_cast<double>(most), &ignored);
+        }
+        const int which = both ? 1 : 0;
+        if (PHASE == 3) {
+            if (both && k_bin >= 0) gather<LIST>(rec.list[0], &rec.count[0], row, from, [&](float x) { return in_range(x, k_bin, k_bin); });
+            if (second >= 0) gather<LIST>(rec.list[which], &rec.count[which], row, from, [&](float x) { return in_range(x, first, second); });
+            // kept mass of the part's scores above those
+            const Kept kept(0, from, s.min_p);
+            const int end = second >= 0 ? first : BINS;
+            double sum = 0.0;
+            row.template each<1>([&](int at, const typename ROW::vec& v) {
+                if (!ROW::any(v, st.lo)) return;
+#pragma unroll
+                for (int e = 0; e < ROW::E; ++e) {
+                    const float x = static_cast<float>(v[e]);
+                    const double w = kept(st.w, x, at + e);
+                    sum += ((x >= st.lo) & (st.template bin<BINS>(x) < end)) ? w : 0.0;
+                }
+            });
+            const uint64_t all = block_sum<WAVES>(sh.part, Weights::whole_units(sum));
+            if (t == 0) rec.kept[part] = all;
+        } else {
+            one_workgroup = rec.count[0] > LIST || (both && rec.count[1] > LIST);
+            if (!one_workgroup) {
+                uint64_t last = 0;
+                if (both && k_bin >= 0) {
+                    uint64_t in_list;
+                    fetch_list(0);
+                    last = last_in_list<THREADS>(sh, st.w, static_cast<int>(rec.count[0]), false, k_above, s.k, &in_list);
+                    k_mass += in_list;
+                }
+                int count = 0;
+                if (second >= 0) {
+                    const double target = both ? s.p * static_cast<double>(k_mass) : s.k ? s.k : s.p * static_cast<double>(mass_before(BINS));
+                    above = s.k && !both ? k_above : mass_before(first);
+                    __syncthreads();
+                    fetch_list(which);
+                    count = static_cast<int>(rec.count[which]);
+                    last = last_in_list<THREADS>(sh, st.w, count, s.p < 1.0, above, target, &ignored);
+                }
+                if (t < plan.parts) sh.mass[t] = rec.kept[t];
+                __syncthreads();
+                for (int j = t; j < count; j += THREADS) {   // the list's kept entries, to their parts
+                    const uint64_t e = sh.sorted[j];
+                    const double raw = st.w.raw(entry_score(e));
+                    if (e >= last && raw >= s.min_p * kUnits) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[entry_index(e) / plan.len]), static_cast<unsigned long long>(Weights::whole_units(rint(raw))));
+                }
+                __syncthreads();
+                return draw_in_part(last);
+            }
+        }
+    }
+    if (PHASE == last_phase && one_workgroup && part == 0) {
+        __syncthreads();
+        whole_row<T, THREADS>(sh, a, r);
+    }
+}
+
+template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows, void* work, hipStream_t st)
 {
     constexpr int E = 16 / sizeof(T);
+    const SplitPlan plan = split_plan(rows, a.n);
     const dim3 grid(static_cast<unsigned>(rows));
+    if (plan.parts > 1) {
+        const int phases = a.top_k || a.top_p ? 4 : 3;
+        const dim3 parts(static_cast<unsigned>(plan.parts), static_cast<unsigned>(rows));
+        SplitRow* records = static_cast<SplitRow*>(work);
+        void (*kernels[4])(PolicyArgs, SplitPlan, SplitRow*, int) = {policy_split_kernel<T, 1>, policy_split_kernel<T, 2>, policy_split_kernel<T, 3>, policy_split_kernel<T, 4>};
+        for (int p = 0; p < phases; ++p) {
+            hipLaunchKernelGGL(kernels[p], parts, dim3(kPartThreads), 0, st, a, plan, records, phases);
+            DQN_LAUNCH_CHECK();
+        }
+        return DQN_OK;
+    }
     if (a.n <= 64) hipLaunchKernelGGL(policy_short_kernel<T>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, rows);
     else if (a.n <= 256 * E * 8) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL((policy_row_kernel<T, 1024>), grid, dim3(1024), 0, st, a);
+    DQN_LAUNCH_CHECK();
+    return DQN_OK;
 }
 
 int enqueue_policy_sample(const PolicyArgs& a, int32_t type, int64_t rows, void* work, hipStream_t st)
 {
-    (void)work;
-    type == DQN_TYPE_FP32 ? launch_policy<float>(a, rows, st) : type == DQN_TYPE_BF16 ? launch_policy<bf16_t>(a, rows, st) : launch_policy<_Float16>(a, rows, st);
-    DQN_LAUNCH_CHECK();
-    return DQN_OK;
+    return type == DQN_TYPE_FP32 ? launch_policy<float>(a, rows, work, st) : type == DQN_TYPE_BF16 ? launch_policy<bf16_t>(a, rows, work, st) : launch_policy<_Float16>(a, rows, work, st);
 }
 
 }  // namespace dqn
@@ -751,8 +977,8 @@ extern "C" {
 
 size_t policy_sample_workspace(int64_t rows, int64_t n)
 {
-    (void)rows; (void)n;
-    return 0;
+    if (rows < 1 || rows > POLICY_SAMPLE_MAX_ROWS || n < 1 || n > POLICY_SAMPLE_MAX_N || split_plan(rows, n).parts == 1) return 0;
+    return static_cast<size_t>(rows) * sizeof(SplitRow);
 }
 
 int policy_sample(const void* scores, int32_t type, int64_t ld, int64_t rows, int64_t n, const float* temperature, const int32_t* top_k, const float* top_p,
