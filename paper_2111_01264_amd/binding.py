@@ -61,6 +61,9 @@ EXPORTS = {
                           C.c_void_p, C.c_void_p]),
     "dqn_act_static": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_float, C.c_uint64, C.c_int32,
                                  C.c_void_p, C.c_void_p]),
+    "dqn_act_sampled": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_uint64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "dqn_quantize_actor": (C.c_int, [C.c_void_p, C.c_int32]),
     "dqn_train_step": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
                                  C.c_void_p, C.c_int32, C.c_void_p]),
     "dqn_get_train_q": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
@@ -204,6 +207,18 @@ def dqn_act(ctx, states, W, epsilon, act_step, use_target, actions, q_out=None):
 
 def dqn_act_static(ctx, states, W, epsilon, act_step, use_target, actions, q_out=None):
     _check(_lib.dqn_act_static(ctx, _ptr(states), W, epsilon, act_step, use_target, _ptr(actions), _ptr(q_out)))
+
+
+def dqn_act_sampled(ctx, states, W, temperature, top_k, top_p, min_p, u, act_step, use_target, quantized, actions, q_out=None,
+                    logp=None):
+    f32 = torch.float32
+    _check(_lib.dqn_act_sampled(ctx, _ptr(states), W, _vec(temperature, f32), _vec(top_k, torch.int32), _vec(top_p, f32),
+                                _vec(min_p, f32), _vec(u, f32), act_step, use_target, quantized, _vec(actions, torch.int32),
+                                _vec(q_out, f32), _vec(logp, f32)))
+
+
+def dqn_quantize_actor(ctx, use_target):
+    _check(_lib.dqn_quantize_actor(ctx, use_target))
 
 
 def dqn_train_step(ctx, s, a, r, s2, done, B, loss_out=None):

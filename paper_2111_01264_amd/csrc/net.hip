@@ -22,6 +22,8 @@
 #include "wgrad_all.h"
 #include "wgrad_f32.h"
 #include "head_kernels.h"
+#include "policy.h"
+#include "quant.h"
 
 namespace dqn {
 
@@ -126,6 +128,12 @@ struct dqn_ctx {
     uint64_t pre_step = 0, pre_epoch = 0;
     int last_B = 0;
     int num_cus = 256;
+    // the quantised actor (dqn_quantize_actor): levels and scales of fc1.w [512][3136] and fc2.w [A][512] (device layout), and the act step's intermediates
+    int8_t *q8_w1 = nullptr, *q8_w2 = nullptr, *q8_x = nullptr, *q8_h = nullptr;
+    float *q8_s1 = nullptr, *q8_s2 = nullptr, *q8_sx = nullptr, *q8_sh = nullptr, *q8_hidden = nullptr;
+    // theta (0) and theta^- (1) change: how often they have, and at which count the levels were made (0: never).  Those of theta are read and written under online_mu.
+    std::atomic<uint64_t> changes[2] = {{1}, {1}};
+    uint64_t q8_at[2] = {0, 0};
     // per-kernel timing (dqn_profile_*)
     int prof_id = 0;
     std::vector<hipEvent_t> prof_events;   // pairs
@@ -230,11 +238,11 @@ __global__ __launch_bounds__(256) void sample_desc_kernel(GatherPlan plan, int32
 }
 
 // Forward pass of `groups` independent (input, parameter set) pairs with n samples each, up to the
-// fc1 k-slices.
+// fc1 k-slices (tower_only: up to conv3's output, ws.act3).
 template <typename T>
 static int forward_to_fc1(dqn_ctx* c, hipStream_t st, Workspace& ws, int groups, const uint8_t* const* x,
                           const void* const* shadow, const float* const* master, int n, bool timed,
-                          const PushStepPlan* push = nullptr, const StateSource* src = nullptr)
+                          const PushStepPlan* push = nullptr, const StateSource* src = nullptr, bool tower_only = false)
 {
     const Offsets& o = c->off;
     auto pp = [&](int id) { return timed ? prof_pair(c, id) : ProfPair(); };
@@ -312,6 +320,7 @@ static int forward_to_fc1(dqn_ctx* c, hipStream_t st, Workspace& ws, int groups,
                      a.w1[0], a.w2[0], a);
         DQN_LAUNCH_CHECK();
     }
+    if (tower_only) return DQN_OK;
     // fc1 as k-slices of fp32 partial sums [groups][slices][n][512]; the head kernel adds them
     if (n <= 32) {
         FcSkArgs<T> a{};
@@ -378,6 +387,27 @@ static int act_impl(dqn_ctx* c, Workspace& ws, const uint8_t* states, int W, flo
                        ha.w2[0], ha.b1[0], ha.b2[0], ha.epsilon, ha);
     DQN_LAUNCH_CHECK();
     return DQN_OK;
+}
+
+// Q rows [W][A] of the quantised actor: the conv layers as ever, then fc1 and fc2 on 8-bit levels, each input row quantised with a scale of its own.
+template <typename T>
+static int q8_rows(dqn_ctx* c, const uint8_t* states, int W, int use_target, float* q)
+{
+    const Offsets& o = c->off;
+    hipStream_t st = c->act_stream;
+    const uint8_t* x[1] = {states};
+    const void* shadow[1] = {use_target ? c->sh_t : c->sh};
+    const float* master[1] = {use_target ? c->theta_t : c->theta};
+    int rc = forward_to_fc1<T>(c, st, c->act_ws, 1, x, shadow, master, W, false, nullptr, nullptr, true);
+    if (rc != DQN_OK) return rc;
+    constexpr int kType = std::is_same<T, bf16_t>::value ? DQN_TYPE_BF16 : DQN_TYPE_FP32;
+    rc = enqueue_quantize_rows(c->act_ws.act3, kType, 3136, W, 3136, c->q8_x, 3136, c->q8_sx, nullptr, 0, st);
+    if (rc != DQN_OK) return rc;
+    rc = enqueue_q8_linear(c->q8_x, 3136, c->q8_sx, c->q8_w1, 3136, c->q8_s1, master[0] + o.bf1, true, W, 512, 3136, c->q8_hidden, DQN_TYPE_FP32, 512, st);
+    if (rc != DQN_OK) return rc;
+    rc = enqueue_quantize_rows(c->q8_hidden, DQN_TYPE_FP32, 512, W, 512, c->q8_h, 512, c->q8_sh, nullptr, 0, st);
+    if (rc != DQN_OK) return rc;
+    return enqueue_q8_linear(c->q8_h, 512, c->q8_sh, c->q8_w2, 512, c->q8_s2, master[0] + o.bf2, false, W, c->A, 512, q, DQN_TYPE_FP32, c->A, st);
 }
 
 template <typename T>
@@ -683,6 +713,16 @@ int dqn_create(const dqn_config* cfg, void* act_stream, void* train_stream, dqn_
         DQN_HIP(hipMalloc((void**)&c->dqv, B * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->lossv, B * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->loss_keep, sizeof(float)));
+        const size_t E = cfg->max_envs, A = c->A;
+        DQN_HIP(hipMalloc((void**)&c->q8_w1, 512 * 3136));
+        DQN_HIP(hipMalloc((void**)&c->q8_w2, A * 512));
+        DQN_HIP(hipMalloc((void**)&c->q8_x, E * 3136));
+        DQN_HIP(hipMalloc((void**)&c->q8_h, E * 512));
+        DQN_HIP(hipMalloc((void**)&c->q8_s1, 512 * sizeof(float)));
+        DQN_HIP(hipMalloc((void**)&c->q8_s2, A * sizeof(float)));
+        DQN_HIP(hipMalloc((void**)&c->q8_sx, E * sizeof(float)));
+        DQN_HIP(hipMalloc((void**)&c->q8_sh, E * sizeof(float)));
+        DQN_HIP(hipMalloc((void**)&c->q8_hidden, E * 512 * sizeof(float)));
         for (int i = 0; i < 2; ++i) {
             DQN_HIP(hipMalloc((void**)&c->mb_s[i], B * kStateBytes));
             DQN_HIP(hipMalloc((void**)&c->mb_s2[i], B * kStateBytes));
@@ -720,6 +760,8 @@ int dqn_destroy(dqn_ctx* c)
     (void)hipFree(c->dzh); (void)hipFree(c->dz3); (void)hipFree(c->dz2); (void)hipFree(c->dz1);
     (void)hipFree(c->dqv); (void)hipFree(c->lossv); (void)hipFree(c->loss_keep);
     (void)hipFree(c->bsh); (void)hipFree(c->bias_partial); (void)hipFree(c->wg_partial);
+    (void)hipFree(c->q8_w1); (void)hipFree(c->q8_w2); (void)hipFree(c->q8_x); (void)hipFree(c->q8_h); (void)hipFree(c->q8_s1); (void)hipFree(c->q8_s2);
+    (void)hipFree(c->q8_sx); (void)hipFree(c->q8_sh); (void)hipFree(c->q8_hidden);
     for (int i = 0; i < 2; ++i) {
         (void)hipFree(c->mb_s[i]); (void)hipFree(c->mb_s2[i]); (void)hipFree(c->mb_a[i]); (void)hipFree(c->mb_r[i]); (void)hipFree(c->mb_d[i]);
         (void)hipFree(c->mb_desc[i]);
@@ -749,6 +791,7 @@ int dqn_set_params(dqn_ctx* c, int which, const float* host_src, size_t n)
     DQN_LAUNCH_CHECK();
     if (which == DQN_PARAMS_ONLINE || which == DQN_PARAMS_TARGET) {   // the network's operand copies (backward ones: theta only)
         const bool online = which == DQN_PARAMS_ONLINE;
+        c->changes[online ? 0 : 1].fetch_add(1, std::memory_order_acq_rel);
         void *sh = online ? c->sh : c->sh_t, *bsh = online ? c->bsh : nullptr;
         if (c->cfg.precision == DQN_PRECISION_BF16)
             hipLaunchKernelGGL(build_copies_kernel<bf16_t>, dim3(blocks), dim3(256), 0, c->train_stream, dst, static_cast<bf16_t*>(sh), static_cast<bf16_t*>(bsh), c->off);
@@ -855,6 +898,62 @@ int dqn_act_push_step(dqn_ctx* c, replay* rb, const uint8_t* push_frames, const 
     return DQN_OK;
 }
 
+int dqn_quantize_actor(dqn_ctx* c, int32_t use_target)
+{
+    if (!c) return fail(DQN_EINVAL, "dqn_quantize_actor: ctx is null");
+    const int which = use_target ? 1 : 0;
+    std::unique_lock<std::mutex> online_lock(c->online_mu, std::defer_lock);
+    if (!use_target) {
+        online_lock.lock();
+        DQN_HIP(wait_for_train(c));
+    }
+    c->q8_at[0] = c->q8_at[1] = 0;   // (the buffers hold one network's levels)
+    const float* theta = use_target ? c->theta_t : c->theta;
+    int rc = enqueue_quantize_rows(theta + c->off.wf1, DQN_TYPE_FP32, 3136, 512, 3136, c->q8_w1, 3136, c->q8_s1, nullptr, 0, c->act_stream);
+    if (rc != DQN_OK) return rc;
+    rc = enqueue_quantize_rows(theta + c->off.wf2, DQN_TYPE_FP32, 512, c->A, 512, c->q8_w2, 512, c->q8_s2, nullptr, 0, c->act_stream);
+    if (rc != DQN_OK) return rc;
+    c->q8_at[which] = c->changes[which].load(std::memory_order_acquire);
+    if (!use_target) {
+        DQN_HIP(hipEventRecord(c->ev_act, c->act_stream));
+        c->act_reads_online.store(true, std::memory_order_release);
+    }
+    return DQN_OK;
+}
+
+int dqn_act_sampled(dqn_ctx* c, const uint8_t* states, int32_t W, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    const float* u, uint64_t act_step, int32_t use_target, int32_t quantized, int32_t* actions, float* q_out, float* logp)
+{
+    const char* who = "dqn_act_sampled";
+    if (!c) return fail(DQN_EINVAL, "%s: ctx is null", who);
+    if (W < 1 || W > c->cfg.max_envs) return fail(DQN_EINVAL, "%s: W = %d outside 1..%d", who, W, c->cfg.max_envs);
+    if (!states || !actions) return fail(DQN_EINVAL, "%s: null pointer", who);
+    if (!aligned16(states)) return fail(DQN_EINVAL, "%s: states not 16-byte aligned", who);
+    for (const void* p : {static_cast<const void*>(temperature), static_cast<const void*>(top_k), static_cast<const void*>(top_p), static_cast<const void*>(min_p),
+                          static_cast<const void*>(u), static_cast<const void*>(actions), static_cast<const void*>(q_out), static_cast<const void*>(logp)})
+        if (!aligned_to(p, 4)) return fail(DQN_EINVAL, "%s: a pointer is not aligned to its elements", who);
+    const int which = use_target ? 1 : 0;
+    std::unique_lock<std::mutex> online_lock(c->online_mu, std::defer_lock);
+    if (!use_target) online_lock.lock();
+    if (quantized && c->q8_at[which] != c->changes[which].load(std::memory_order_acquire))
+        return fail(DQN_ESTATE, "%s: dqn_quantize_actor has not run since these parameters changed", who);
+    if (!use_target) DQN_HIP(wait_for_train(c));
+    float* q = q_out ? q_out : c->act_ws.q;
+    const bool bf16 = c->cfg.precision == DQN_PRECISION_BF16;
+    int rc;
+    if (quantized) rc = bf16 ? q8_rows<bf16_t>(c, states, W, use_target, q) : q8_rows<float>(c, states, W, use_target, q);
+    else rc = bf16 ? act_impl<bf16_t>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q) : act_impl<float>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q);
+    if (rc != DQN_OK) return rc;
+    const PolicyArgs pa{q, c->A, c->A, temperature, top_k, top_p, min_p, u, c->cfg.seed, act_step, actions, logp};
+    rc = enqueue_policy_sample(pa, DQN_TYPE_FP32, W, nullptr, c->act_stream);   // (rows this short need no workspace)
+    if (rc != DQN_OK) return rc;
+    if (!use_target) {
+        DQN_HIP(hipEventRecord(c->ev_act, c->act_stream));
+        c->act_reads_online.store(true, std::memory_order_release);
+    }
+    return DQN_OK;
+}
+
 int dqn_train_step(dqn_ctx* c, const uint8_t* s, const int32_t* a, const float* r, const uint8_t* s2,
                    const float* done, int32_t B, float* loss_out)
 {
@@ -868,6 +967,7 @@ int dqn_train_step(dqn_ctx* c, const uint8_t* s, const int32_t* a, const float* 
     if (c->cfg.precision == DQN_PRECISION_BF16) rc = train_impl<bf16_t>(c, s, a, r, s2, done, B, loss_out);
     else rc = train_impl<float>(c, s, a, r, s2, done, B, loss_out);
     if (rc != DQN_OK) return rc;
+    c->changes[0].fetch_add(1, std::memory_order_acq_rel);
     c->train_unrecorded.store(true, std::memory_order_release);   // the event is recorded by the first reader, if any
     c->last_B = B;
     return DQN_OK;
@@ -913,6 +1013,7 @@ int dqn_train_step_sampled(dqn_ctx* c, replay* rb, int32_t B, uint64_t sample_st
     auto train = c->cfg.precision == DQN_PRECISION_BF16 ? train_impl<bf16_t> : train_impl<float>;
     rc = train(c, c->mb_s[buf], c->mb_a[buf], c->mb_r[buf], c->mb_s2[buf], c->mb_d[buf], B, loss_out, ride, ride_desc, by_desc ? &src : nullptr);
     if (rc != DQN_OK) return rc;
+    c->changes[0].fetch_add(1, std::memory_order_acq_rel);
     c->train_unrecorded.store(true, std::memory_order_release);
     c->last_B = B;
     if (ride) {
@@ -1000,6 +1101,7 @@ int dqn_sync_target(dqn_ctx* c, replay* rb, int32_t blocking)
     else
         hipLaunchKernelGGL(target_copy_kernel<float>, grid, block, 0, c->train_stream, c->theta, c->theta_t, static_cast<const float*>(c->sh), static_cast<float*>(c->sh_t), n, n_copy);
     DQN_LAUNCH_CHECK();
+    c->changes[1].fetch_add(1, std::memory_order_acq_rel);
     DQN_HIP(hipEventRecord(c->ev_sync, c->train_stream));
     DQN_HIP(hipStreamWaitEvent(c->act_stream, c->ev_sync, 0));
     if (blocking) DQN_HIP(hipStreamSynchronize(c->train_stream));
