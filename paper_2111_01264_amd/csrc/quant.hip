@@ -1,5 +1,5 @@
 // 8-bit levels with a scale for each row, and the product of two such matrices (include/dqn_mi355.h: q8_quantize_rows, q8_linear).
-#include <mutex>
+#include <atomic>
 #include <type_traits>
 
 #include "quant.h"
@@ -333,12 +333,12 @@ __device__ inline void q8_to_lds(const int8_t* base, uint32_t offset, uint32_t l
 }
 template <int LEFT> __device__ inline void q8_wait() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory"); }
 
-template <typename T, int TILE, bool ALIGNED>
-__global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void q8_tile_kernel(Q8Args a, int tiles_m, int tiles_n)
+template <typename T, int TILE, int THREADS, bool ALIGNED>
+__global__ __launch_bounds__(THREADS, TILE == 256 ? THREADS / 256 : TILE == 128 ? 2 : 4) void q8_tile_kernel(Q8Args a, int tiles_m, int tiles_n)
 {
-    constexpr int F = TILE / 64;                                   // 32-row operand tiles per wavefront and side
+    constexpr int WN = THREADS / 128, FX = TILE / 64, FW = TILE / WN / 32;   // the wavefronts' parts: WN along n, two along m; 32-row operand tiles of each
     constexpr int kHalf = TILE * kStep, kStage = 2 * kHalf;        // bytes: w's rows, then x's
-    constexpr int L = kStage / 16 / 256;                           // 16-byte loads per thread and step
+    constexpr int L = kStage / 16 / THREADS;                          // 16-byte loads per thread and step
     extern __shared__ __attribute__((aligned(128))) int8_t q8_smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // Workgroups go to the eight XCDs in turn, each with an L2 of its own: an XCD takes a contiguous eighth of the tiles, in strips of eight
@@ -352,11 +352,11 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void q8_tile_kernel(Q8Arg
         tn = static_cast<int>(in / rows);
     }
     const int m0 = tm * TILE, n0 = tn * TILE, K = a.K;
-    // this thread's chunks of a stage: rows (tid >> 2) + 64 j of w, then of x
+    // this thread's chunks of a stage: rows (tid >> 2) + THREADS / 4 * j of w, then of x
     const int row = tid >> 2, chunk = (tid & 3) ^ q8_swizzle(tid >> 2);
     const int8_t* wb = a.w + static_cast<int64_t>(n0) * a.ldw;
     const int8_t* xb = a.x + static_cast<int64_t>(m0) * a.ldx;
-    auto row_of = [&](int j) { return j < L / 2 ? min(row + 64 * j, a.N - 1 - n0) : min(row + 64 * (j - L / 2), a.M - 1 - m0); };   // (past the end: the last one again)
+    auto row_of = [&](int j) { return j < L / 2 ? min(row + THREADS / 4 * j, a.N - 1 - n0) : min(row + THREADS / 4 * (j - L / 2), a.M - 1 - m0); };   // (past the end: the last one again)
     uint32_t offset[L];
     const int8_t* ptr[L];
 #pragma unroll
@@ -365,111 +365,144 @@ __global__ __launch_bounds__(256, TILE == 256 ? 1 : 2) void q8_tile_kernel(Q8Arg
         else ptr[j] = j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx;
     }
     const uint32_t lds0 = static_cast<uint32_t>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) int8_t*)q8_smem));
-    auto request = [&](int step) {   // ALIGNED
-        const uint32_t to = lds0 + (step % kStages) * kStage + wave * 1024;
+    auto request_one = [&](int place, const int8_t* from, int j) {   // ALIGNED
+        q8_to_lds(from, offset[j], lds0 + (place % kStages) * kStage + wave * 1024 + j * (16 * THREADS));
+    };
+    auto request = [&](int place, int step) {
 #pragma unroll
-        for (int j = 0; j < L; ++j) q8_to_lds((j < L / 2 ? wb : xb) + static_cast<int64_t>(step) * kStep, offset[j], to + j * 4096);
+        for (int j = 0; j < L; ++j) request_one(place, (j < L / 2 ? wb : xb) + static_cast<int64_t>(step) * kStep, j);
     };
     i32x4 reg[ALIGNED ? 1 : L];
     auto fetch = [&](int step) {   // not ALIGNED
+        const int k = step * kStep + 16 * chunk;
+        if (step < K / kStep) {
 #pragma unroll
-        for (int j = 0; j < L; ++j) reg[j] = q8_load(ptr[j], step * kStep + 16 * chunk, K, true);
+            for (int j = 0; j < L; ++j) __builtin_memcpy(&reg[j], ptr[j] + k, 16);
+        } else {
+#pragma unroll
+            for (int j = 0; j < L; ++j) reg[j] = q8_load(ptr[j], k, K, true);
+        }
     };
     auto put = [&](int step) {
 #pragma unroll
-        for (int j = 0; j < L; ++j) *reinterpret_cast<i32x4*>(q8_smem + (step % kStages) * kStage + j * 4096 + tid * 16) = reg[j];
+        for (int j = 0; j < L; ++j) *reinterpret_cast<i32x4*>(q8_smem + (step % kStages) * kStage + j * (16 * THREADS) + tid * 16) = reg[j];
     };
     // reads: rows 32 i + lane % 32 of this wavefront's part, chunks 2 h and 2 h + 1
-    const int lr = lane & 31, lc = lane >> 5, wn = (wave & 1) * (TILE / 2), wm = (wave >> 1) * (TILE / 2);
+    const int lr = lane & 31, lc = lane >> 5, wn = (wave >> 1) * (TILE / WN), wm = (wave & 1) * (TILE / 2);
     const int sw = q8_swizzle(lr);
     const int at_w = (wn + lr) * kStep, at_x = kHalf + (wm + lr) * kStep;
-    i32x4 wf[2][F], xf[2][F];
-    auto read = [&](int step, int h) {
+    i32x4 wf[2][FW], xf[2][FX];
+    auto read_one = [&](int step, int h, int q) {
         const int8_t* st = q8_smem + (step % kStages) * kStage + 16 * ((2 * h + lc) ^ sw);
-#pragma unroll
-        for (int i = 0; i < F; ++i) wf[h][i] = *reinterpret_cast<const i32x4*>(st + at_w + i * 32 * kStep);
-#pragma unroll
-        for (int i = 0; i < F; ++i) xf[h][i] = *reinterpret_cast<const i32x4*>(st + at_x + i * 32 * kStep);
+        const int i = q < FW ? q : q - FW;
+        (q < FW ? wf[h][i % FW] : xf[h][i % FX]) = *reinterpret_cast<const i32x4*>(st + (q < FW ? at_w : at_x) + i * 32 * kStep);
     };
-    i32x16 acc[F][F];
+    auto read = [&](int step, int h) {
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+        for (int q = 0; q < FW + FX; ++q) read_one(step, h, q);
+    };
+    i32x16 acc[FW][FX];
 #pragma unroll
-        for (int j = 0; j < F; ++j)
+    for (int i = 0; i < FW; ++i)
+#pragma unroll
+        for (int j = 0; j < FX; ++j)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[i][j][v] = 0;
-    auto multiply = [&](int h) {
+    // The products of half step h, and between them the reads of the next half step (issued during the first half of the products) and the requests of a later
+    // stage (during the second): a wavefront issues in order, and what it issues in one go it does not multiply meanwhile.
+    auto multiply = [&](int h, auto&& read_q, auto&& request_j) {
 #pragma unroll
-        for (int i = 0; i < F; ++i)
+        for (int n = 0; n < FW * FX; ++n) {
+            acc[n / FX][n % FX] = q8_mma(wf[h][n / FX], xf[h][n % FX], acc[n / FX][n % FX]);
 #pragma unroll
-            for (int j = 0; j < F; ++j) acc[i][j] = q8_mma(wf[h][i], xf[h][j], acc[i][j]);
+            for (int q = 0; q < FW + FX; ++q)
+                if (q * FW * FX / (2 * (FW + FX)) == n) read_q(q);
+#pragma unroll
+            for (int j = 0; j < L; ++j)
+                if (j * FW * FX / L == n) request_j(j);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     };
-    // ALIGNED: whole steps through LDS directly, a last partial one through registers, which cut it off at K
-    const int steps = ALIGNED ? K / kStep : (K + kStep - 1) / kStep;
+    auto nothing = [](int) {};
+    // ALIGNED: pairs of whole steps through LDS directly, the rest through registers, which cut it off at K
+    static_assert(kStages == 4, "two pairs of steps");
+    const int steps = ALIGNED ? K / (2 * kStep) * 2 : (K + kStep - 1) / kStep;
     if (steps > 0) {
         if constexpr (ALIGNED) {
+            // Two steps at a time: what they need of a row is one cache line, requested as a whole.  One loop without branches: the last steps request the last stage again, and
+            // read what nobody uses, so that the number of loads in flight is the same in all.
 #pragma unroll
-            for (int s = 0; s < kStages; ++s)
-                if (s < steps) request(s);
-            if (steps >= kStages) q8_wait<(kStages - 1) * L>(); else q8_wait<0>();
+            for (int s = 0; s < kStages; ++s) request(s, min(s & ~1, steps - 2) + (s & 1));
+            q8_wait<(kStages - 1) * L>();
+            read(0, 0);
+            for (int s = 0; s < steps; s += 2) {
+                multiply(0, [&](int q) { read_one(s, 1, q); }, nothing);
+                q8_wait<2 * L>();
+                multiply(1, [&](int q) { read_one(s + 1, 0, q); }, nothing);
+                multiply(0, [&](int q) { read_one(s + 1, 1, q); }, nothing);
+                q8_wait<0>();   // (the two steps' loads alternate: the next step's are not complete before the one's after it)
+                const int64_t next = static_cast<int64_t>(min(s + 4, steps - 2)) * kStep;   // (stages s + 4 and s + 5 take the places of s and s + 1)
+                multiply(1, [&](int q) { read_one(s + 2, 0, q); }, [&](int j) {
+                    request_one(s, (j < L / 2 ? wb : xb) + next, j);
+                    request_one(s + 1, (j < L / 2 ? wb : xb) + next + kStep, j);
+                });
+            }
+            q8_wait<0>();
         } else {
             for (int s = 0; s < kStages - 1; ++s)
                 if (s < steps) { fetch(s); put(s); }
             if (kStages - 1 < steps) fetch(kStages - 1);
             __syncthreads();
-        }
-        read(0, 0);
-        for (int s = 0; s < steps; ++s) {
-            read(s, 1);
-            multiply(0);
-            if (s + 1 < steps) {
-                if constexpr (ALIGNED) {
-                    if (s + kStages <= steps) q8_wait<(kStages - 2) * L>(); else q8_wait<0>();
-                    if (s + kStages < steps) request(s + kStages);
-                } else {
-                    if (s + kStages - 1 < steps) put(s + kStages - 1);
-                    __syncthreads();
-                    if (s + kStages < steps) fetch(s + kStages);
-                }
-                read(s + 1, 0);
+            read(0, 0);
+            for (int s = 0; s < steps; ++s) {
+                multiply(0, [&](int q) { read_one(s, 1, q); }, nothing);
+                if (s + kStages - 1 < steps) put(s + kStages - 1);
+                __syncthreads();
+                if (s + kStages < steps) fetch(s + kStages);
+                multiply(1, [&](int q) { read_one(s + 1, 0, q); }, nothing);   // (behind the last step: what nobody uses)
             }
-            multiply(1);
         }
     }
-    if (ALIGNED && steps * kStep < K) {
-        __syncthreads();
+    if constexpr (ALIGNED) {
+        for (int k = steps * kStep; k < K; k += kStep) {
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < L; ++j) {
-            const int8_t* p = (j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx);
-            *reinterpret_cast<i32x4*>(q8_smem + j * 4096 + tid * 16) = q8_load(p, steps * kStep + 16 * chunk, K, true);
+            for (int j = 0; j < L; ++j) {
+                const int8_t* p = (j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx);
+                *reinterpret_cast<i32x4*>(q8_smem + j * (16 * THREADS) + tid * 16) = q8_load(p, k + 16 * chunk, K, true);
+            }
+            __syncthreads();
+            read(0, 0); read(0, 1);
+            multiply(0, nothing, nothing); multiply(1, nothing, nothing);
         }
-        __syncthreads();
-        read(0, 0); read(0, 1);
-        multiply(0); multiply(1);
     }
-    float sx[F];
+    float sx[FX];
 #pragma unroll
-    for (int j = 0; j < F; ++j) sx[j] = a.sx[min(m0 + wm + 32 * j + lr, a.M - 1)];
+    for (int j = 0; j < FX; ++j) sx[j] = a.sx[min(m0 + wm + 32 * j + lr, a.M - 1)];
 #pragma unroll
-    for (int i = 0; i < F; ++i)
+    for (int i = 0; i < FW; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
             const Q8Columns c = q8_columns(a, n0 + wn + 32 * i + 8 * g + 4 * lc);
 #pragma unroll
-            for (int j = 0; j < F; ++j)
+            for (int j = 0; j < FX; ++j)
                 q8_store<T>(a, c, m0 + wm + 32 * j + lr, sx[j], acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]);
         }
 }
 
-template <typename T, int TILE, bool ALIGNED> static int launch_tile(const Q8Args& a, hipStream_t st)
+template <typename T, int TILE, int THREADS, bool ALIGNED> static int launch_tile(const Q8Args& a, hipStream_t st)
 {
     constexpr int smem = 2 * TILE * kStep * kStages;
-    static std::once_flag once;
-    static hipError_t raised = hipSuccess;
-    std::call_once(once, [] { raised = hipFuncSetAttribute(reinterpret_cast<const void*>(q8_tile_kernel<T, TILE, ALIGNED>), hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
-    DQN_HIP(raised);
+    static std::atomic<uint64_t> raised{0};   // devices whose limit on dynamic LDS has been raised for this kernel
+    int device = 0;
+    DQN_HIP(hipGetDevice(&device));
+    const uint64_t bit = 1ull << (device & 63);
+    if (!(raised.load(std::memory_order_relaxed) & bit)) {
+        DQN_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(q8_tile_kernel<T, TILE, THREADS, ALIGNED>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
+        raised.fetch_or(bit, std::memory_order_relaxed);
+    }
     const int tm = (a.M + TILE - 1) / TILE, tn = (a.N + TILE - 1) / TILE;
-    hipLaunchKernelGGL((q8_tile_kernel<T, TILE, ALIGNED>), dim3(static_cast<unsigned>(tm) * tn), dim3(256), smem, st, a, tm, tn);
+    hipLaunchKernelGGL((q8_tile_kernel<T, TILE, THREADS, ALIGNED>), dim3(static_cast<unsigned>(tm) * tn), dim3(THREADS), smem, st, a, tm, tn);
     DQN_LAUNCH_CHECK();
     return DQN_OK;
 }
@@ -477,23 +510,22 @@ template <typename T, int TILE, bool ALIGNED> static int launch_tile(const Q8Arg
 template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
 {
     const auto blocks = [&](int bn, int bm) { return dim3(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + bm - 1) / bm)); };
-    if (a.M <= 64) {
-        if (a.M <= 16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 1, 4>), blocks(16, 16), dim3(256), 0, st, a);
-        else if (a.M <= 32) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 2, 4>), blocks(16, 32), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 64), dim3(256), 0, st, a);
+    if (a.M <= 16) {
+        hipLaunchKernelGGL((q8_stream_kernel<T, 16, 1, 8>), blocks(16, 16), dim3(512), 0, st, a);
         DQN_LAUNCH_CHECK();
         return DQN_OK;
     }
-    const int64_t t256 = static_cast<int64_t>((a.M + 255) / 256) * ((a.N + 255) / 256), t128 = static_cast<int64_t>((a.M + 127) / 128) * ((a.N + 127) / 128);
-    if (t128 < 64) {
-        hipLaunchKernelGGL((q8_stream_kernel<T, 32, 1, 4>), blocks(32, 32), dim3(256), 0, st, a);
+    const auto tiles = [&](int64_t t) { return (a.M + t - 1) / t * ((a.N + t - 1) / t); };
+    if (tiles(64) < 128) {
+        hipLaunchKernelGGL((q8_stream_kernel<T, 32, 1, 8>), blocks(32, 32), dim3(512), 0, st, a);
         DQN_LAUNCH_CHECK();
         return DQN_OK;
     }
     // 16-byte loads straight into LDS need rows on 16-byte borders; a lane's place within a tile is a 32-bit offset
     const bool aligned = aligned16(a.x) && aligned16(a.w) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.ldx < (1 << 23) && a.ldw < (1 << 23);
-    if (t256 >= 192) return aligned ? launch_tile<T, 256, true>(a, st) : launch_tile<T, 128, false>(a, st);
-    return aligned ? launch_tile<T, 128, true>(a, st) : launch_tile<T, 128, false>(a, st);
+    if (tiles(128) < 200) return aligned ? launch_tile<T, 64, 256, true>(a, st) : launch_tile<T, 64, 256, false>(a, st);
+    if (tiles(256) < 192) return aligned ? launch_tile<T, 128, 256, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
+    return aligned ? launch_tile<T, 256, 512, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
 }
 
 int enqueue_q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, int64_t ldw, const float* sw, const float* bias, bool relu, int64_t M,
