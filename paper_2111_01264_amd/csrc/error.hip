@@ -1,6 +1,8 @@
 // Thread-local error message behind dqn_last_error(), and the argument checks that calls without a handle share.
 #include "common.h"
 
+#include <mutex>
+
 namespace dqn {
 
 char* error_buffer()
@@ -16,6 +18,24 @@ int fail(int code, const char* fmt, ...)
     vsnprintf(error_buffer(), 512, fmt, ap);
     va_end(ap);
     return code;
+}
+
+hipError_t raise_dynamic_lds(const void* kernel, int bytes)
+{
+    constexpr int kKernels = 64;
+    static std::mutex mu;
+    static struct { const void* kernel; uint64_t devices; } done[kKernels];   // (the library has fewer such kernels)
+    int device = 0;
+    const hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    std::lock_guard<std::mutex> lock(mu);
+    int i = 0;
+    while (i < kKernels && done[i].kernel && done[i].kernel != kernel) ++i;
+    if (i < kKernels && done[i].kernel == kernel && (done[i].devices & bit)) return hipSuccess;
+    const hipError_t r = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (r == hipSuccess && i < kKernels) { done[i].kernel = kernel; done[i].devices |= bit; }
+    return r;
 }
 
 int check_type(const char* who, int32_t type)

@@ -1,4 +1,6 @@
 // Drawing an index from a row of scores under temperature, top-k, top-p and min-p (include/dqn_mi355.h: policy_sample).
+#include <type_traits>
+
 #include "policy.h"
 
 #include "gemm_mfma.h"
@@ -365,12 +367,36 @@ template <int BINS> __device__ inline RowState row_state(const RowSettings& s, f
     return st;
 }
 
-// Largest and smallest score and NaN of the stretch to every thread; the maxima of `groups` (a power of two, 4 to 256) groups of threads into group[].
-template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(RowShared<THREADS>& sh, const ROW& row, float* hi_out, float* low_out, uint32_t* group, int groups)
+// bf16 scores have few values: all those from 2^-24 to 2^8 and their negatives have a place in a table in LDS, so that a long row needs an exponential per value instead of one per
+// score.  Others (rare) are treated one by one.  256 rows of 131072, top-p: 131 -> 103 us; one compute unit's LDS holds one workgroup then, which a row this long fills anyway.
+constexpr int kTablePlaces = 8192;
+__device__ __forceinline__ uint32_t table_place(bf16_t x)   // kTablePlaces or more: none
+{
+    const uint32_t b = __builtin_bit_cast(uint16_t, x), above = (b & 0x7FFFu) - (103u << 7);
+    return above < 4096u ? above | (b >> 15) << 12 : 0xFFFFFFFFu;
+}
+__device__ __forceinline__ float table_score(uint32_t place) { return __uint_as_float((((place & 4095u) + (103u << 7)) | (place >> 12) << 15) << 16); }
+template <typename T> __device__ __forceinline__ uint32_t table_place(T) { return 0xFFFFFFFFu; }
+
+// Largest and smallest score and NaN of the stretch to every thread (and, where there is a table, how often each value occurs into it and in *others whether there are others); the maxima of `groups` (a power of two, 4 to 256) groups of threads into group[].
+template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(RowShared<THREADS>& sh, const ROW& row, float* hi_out, float* low_out, uint32_t* group, int groups,
+                                                                                  uint32_t* counts = nullptr, bool* others = nullptr)
 {
     float hi = -INFINITY, low = INFINITY;
-    bool nan = false;
+    bool nan = false, no_place = false;
+    if (counts) {
+        for (int i = threadIdx.x; i < kTablePlaces; i += THREADS) counts[i] = 0;
+        __syncthreads();
+    }
     row.template each<4>([&](int first, const typename ROW::vec& v) {
+        if (counts) {
+#pragma unroll
+            for (int e = 0; e < ROW::E; ++e) {
+                const uint32_t place = table_place(v[e]);
+                if (place < kTablePlaces) atomicAdd(&counts[place], 1u);
+                else no_place |= static_cast<float>(v[e]) > -INFINITY;   // (minus infinity, also behind the end, has no mass)
+            }
+        }
 #pragma unroll
         for (int e = 0; e < ROW::E; ++e) {
             const float x = static_cast<float>(v[e]);
@@ -395,7 +421,8 @@ template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(Ro
     for (int q = 0; q < ROW::WAVES; ++q) { hi = fmaxf(hi, key_score(static_cast<uint32_t>(sh.part[q]))); low = fminf(low, key_score(static_cast<uint32_t>(sh.part2[q]))); }
     *hi_out = hi;
     *low_out = low;
-    __syncthreads();
+    no_place = __syncthreads_or(no_place);
+    if (others) *others = no_place;
     return nan;
 }
 
@@ -450,11 +477,33 @@ template <int THREADS> __device__ __forceinline__ void draw_from_list(RowShared<
     }
 }
 
-// The histogram of the stretch's scores: mass, entries, or both.
-template <int THREADS, typename ROW> __device__ __forceinline__ void fill_histogram(RowShared<THREADS>& sh, const ROW& row, const RowState& st, bool masses, bool entries)
+// The histogram of the stretch's scores: mass, entries, or both; from the counts of the values where there are such.
+template <int THREADS, typename ROW> __device__ __forceinline__ void fill_histogram(RowShared<THREADS>& sh, const ROW& row, const RowState& st, bool masses, bool entries,
+                                                                                          const uint32_t* counts = nullptr, bool others = false)
 {
     for (int b = threadIdx.x; b < RowShared<THREADS>::BINS; b += THREADS) { sh.mass[b] = 0; sh.entries[b] = 0; }
     __syncthreads();
+    auto add = [&](float x, uint64_t mass, uint32_t count) {
+        const int b = st.template bin<RowShared<THREADS>::BINS>(x);
+        if (masses) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]), static_cast<unsigned long long>(mass));
+        if (entries) atomicAdd(&sh.entries[b], count);
+    };
+    if (counts) {
+        for (int i = threadIdx.x; i < kTablePlaces; i += THREADS) {
+            const float x = table_score(i);
+            if (counts[i] && x >= st.lo) add(x, counts[i] * st.w.units(x), counts[i]);
+        }
+        if (others)
+            row.template each<1>([&](int, const typename ROW::vec& v) {
+#pragma unroll
+                for (int e = 0; e < ROW::E; ++e) {
+                    const float x = static_cast<float>(v[e]);
+                    if (table_place(v[e]) >= kTablePlaces && x >= st.lo) add(x, st.w.units(x), 1u);
+                }
+            });
+        __syncthreads();
+        return;
+    }
     row.template each<1>([&](int, const typename ROW::vec& v) {
         uint64_t u[ROW::E];
         if (!ROW::any(v, st.lo)) return;
@@ -467,11 +516,7 @@ template <int THREADS, typename ROW> __device__ __forceinline__ void fill_histog
 #pragma unroll
         for (int e = 0; e < ROW::E; ++e) {
             const float x = static_cast<float>(v[e]);
-            if (x >= st.lo) {
-                const int b = st.template bin<RowShared<THREADS>::BINS>(x);
-                if (masses) atomicAdd(reinterpret_cast<unsigned long long*>(&sh.mass[b]), static_cast<unsigned long long>(u[e]));
-                if (entries) atomicAdd(&sh.entries[b], 1u);
-            }
+            if (x >= st.lo) add(x, u[e], 1u);
         }
     });
     __syncthreads();
@@ -571,12 +616,17 @@ struct Kept {
 // The draw from a stretch.  total: all kept mass of the row and target what is left of u's share of it where the stretch begins; where total is 0, the stretch is the whole row and both are found here.
 template <int THREADS, typename ROW>
 __device__ __forceinline__ void draw(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r, const ROW& row, int offset, const RowSettings& s, const Weights& w, uint64_t last, uint64_t total,
-                                     uint64_t target)
+                                     uint64_t target, uint64_t* table = nullptr)
 {
     constexpr int WAVES = THREADS / 64, E = ROW::E;
     const Kept kept(last, offset, s.min_p);
     const int t = threadIdx.x, per = (row.trips + 3) / 4;
     uint64_t sums[4] = {0, 0, 0, 0};   // of four groups of this lane's trips
+    if (table) {   // what a score of each value counts, if it is kept
+        __syncthreads();
+        for (int i = t; i < kTablePlaces; i += THREADS) reinterpret_cast<double*>(table)[i] = kept(w, table_score(i), INT32_MIN);
+        __syncthreads();
+    }
     {
         double sum = 0.0;
         int left = per, group = 0;
@@ -588,7 +638,17 @@ __device__ __forceinline__ void draw(RowShared<THREADS>& sh, const PolicyArgs& a
             ++group;
         };
         row.template each<1>([&](int first, const typename ROW::vec& v) {
-            if (ROW::any(v, kept.score)) {
+            if (!ROW::any(v, kept.score)) {
+            } else if (table) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float x = static_cast<float>(v[e]);
+                    if (x > kept.score || (x == kept.score && first + e <= kept.index)) {
+                        const uint32_t place = table_place(v[e]);
+                        sum += place < kTablePlaces ? reinterpret_cast<const double*>(table)[place] : kept(w, x, first + e);
+                    }
+                }
+            } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e) sum += kept(w, static_cast<float>(v[e]), first + e);
             }
@@ -646,14 +706,16 @@ template <int THREADS, typename ROW> __device__ __forceinline__ int first_of(Row
 }
 
 // ---- a row by one workgroup -----------------------------------------------------------------------------------------------
-template <typename T, int THREADS> __device__ __forceinline__ void whole_row(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r)
+template <typename T, int THREADS> __device__ __forceinline__ void whole_row(RowShared<THREADS>& sh, const PolicyArgs& a, int64_t r, uint64_t* table)
 {
     typedef Row<T, THREADS> ROW;
     const ROW row(a, r, 0, a.n);
     const RowSettings s = row_settings(a, r);
     float hi, low;
     const int groups = groups_for(s.k);
-    const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, groups);
+    bool others = false;
+    uint32_t* counts = !s.greedy && (s.k > kListK || (!s.k && s.p < 1.0)) ? reinterpret_cast<uint32_t*>(table) : nullptr;   // (for the histogram)
+    const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, groups, counts, &others);
     const RowState st = row_state<RowShared<THREADS>::BINS>(s, hi, low, nan);
     if (st.way == Way::kRefused) {
         if (threadIdx.x == 0) answer(a, r, -1, not_a_number());
@@ -674,7 +736,7 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
     uint64_t last = 0;
     bool by_digits = st.way == Way::kDigits || st.way == Way::kShortList;
     if (st.way == Way::kRange) {
-        fill_histogram<THREADS>(sh, row, st, s.p < 1.0, s.k > 0);
+        fill_histogram<THREADS>(sh, row, st, s.p < 1.0, s.k > 0, counts, others);
         uint64_t kept_mass = 0;   // of what top-k leaves
 #pragma unroll 1
         for (int filter = s.k ? 0 : 1; filter < (s.p < 1.0 ? 2 : 1) && !by_digits; ++filter) {
@@ -720,14 +782,17 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
         }
         last = max(last, floor);
     }
-    draw<THREADS>(sh, a, r, row, 0, s, st.w, last, 0, 0);
+    draw<THREADS>(sh, a, r, row, 0, s, st.w, last, 0, 0, table);
 }
+
+template <typename T, int THREADS> constexpr bool kWithTable = std::is_same<T, bf16_t>::value && THREADS == 1024;
 
 template <typename T, int THREADS>
 __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a)
 {
     __shared__ RowShared<THREADS> sh;
-    whole_row<T, THREADS>(sh, a, blockIdx.x);
+    extern __shared__ uint64_t policy_table[];   // kTablePlaces, where kWithTable
+    whole_row<T, THREADS>(sh, a, blockIdx.x, kWithTable<T, THREADS> ? policy_table : nullptr);
 }
 
 // ---- few long rows: a row by several workgroups ------------------------------------------------------------------------------
@@ -939,7 +1004,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_split_kernel(PolicyArgs a
     }
     if (PHASE == last_phase && one_workgroup && part == 0) {
         __syncthreads();
-        whole_row<T, THREADS>(sh, a, r);
+        whole_row<T, THREADS>(sh, a, r, nullptr);
     }
 }
 
@@ -961,7 +1026,11 @@ template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows
     }
     if (a.n <= 64) hipLaunchKernelGGL(policy_short_kernel<T>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, rows);
     else if (a.n <= 256 * E * 8) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
-    else hipLaunchKernelGGL((policy_row_kernel<T, 1024>), grid, dim3(1024), 0, st, a);
+    else {
+        constexpr int smem = kWithTable<T, 1024> ? kTablePlaces * static_cast<int>(sizeof(uint64_t)) : 0;
+        if (smem) DQN_HIP(raise_dynamic_lds(reinterpret_cast<const void*>(policy_row_kernel<T, 1024>), smem));
+        hipLaunchKernelGGL((policy_row_kernel<T, 1024>), grid, dim3(1024), smem, st, a);
+    }
     DQN_LAUNCH_CHECK();
     return DQN_OK;
 }

@@ -1,5 +1,4 @@
 // 8-bit levels with a scale for each row, and the product of two such matrices (include/dqn_mi355.h: q8_quantize_rows, q8_linear).
-#include <atomic>
 #include <type_traits>
 
 #include "quant.h"
@@ -493,14 +492,7 @@ __global__ __launch_bounds__(THREADS, TILE == 256 ? THREADS / 256 : TILE == 128 
 template <typename T, int TILE, int THREADS, bool ALIGNED> static int launch_tile(const Q8Args& a, hipStream_t st)
 {
     constexpr int smem = 2 * TILE * kStep * kStages;
-    static std::atomic<uint64_t> raised{0};   // devices whose limit on dynamic LDS has been raised for this kernel
-    int device = 0;
-    DQN_HIP(hipGetDevice(&device));
-    const uint64_t bit = 1ull << (device & 63);
-    if (!(raised.load(std::memory_order_relaxed) & bit)) {
-        DQN_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(q8_tile_kernel<T, TILE, THREADS, ALIGNED>), hipFuncAttributeMaxDynamicSharedMemorySize, smem));
-        raised.fetch_or(bit, std::memory_order_relaxed);
-    }
+    DQN_HIP(raise_dynamic_lds(reinterpret_cast<const void*>(q8_tile_kernel<T, TILE, THREADS, ALIGNED>), smem));
     const int tm = (a.M + TILE - 1) / TILE, tn = (a.N + TILE - 1) / TILE;
     hipLaunchKernelGGL((q8_tile_kernel<T, TILE, THREADS, ALIGNED>), dim3(static_cast<unsigned>(tm) * tn), dim3(THREADS), smem, st, a, tm, tn);
     DQN_LAUNCH_CHECK();
