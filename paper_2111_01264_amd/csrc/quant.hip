@@ -245,71 +245,61 @@ template <typename T> __device__ inline void q8_store(const Q8Args& a, const Q8C
 
 // ---- few rows: the weights are streamed once, from memory straight into the matrix instructions ---------------------------------
 //
-// A workgroup owns BN rows of w and all of MT * BN rows of x (BN = 16: at most 64 rows of x; BN = 32: one tile of 32 of them per
-// workgroup); its wavefronts take every WAVES-th stretch of k and meet in LDS at the end.  No staging: a row of w is used by one
-// wavefront only, and the rows of x come from cache.
-template <typename T, int BN, int MT, int WAVES>
+// A workgroup owns BN rows of w and BN rows of x (BN = 16: all that there are; 32: a tile of them); its wavefronts take every WAVES-th stretch of k
+// and meet in LDS at the end.  No staging: a row of w is used by one wavefront only, and the rows of x come from cache.  Memory's latency bounds it, so a
+// stretch's U loads of either side are requested while the one before is multiplied, and what is left behind the last stretch before anything else.
+template <typename T, int BN, int U, int WAVES>
 __global__ __launch_bounds__(WAVES * 64) void q8_stream_kernel(Q8Args a)
 {
     typedef typename std::conditional<BN == 16, i32x4, i32x16>::type acc_t;
     constexpr int KI = BN == 16 ? 64 : 32, V = BN == 16 ? 4 : 16;   // k of one instruction, results per lane
-    constexpr int U = BN == 16 ? (MT == 1 ? 8 : 4) : 4;             // instructions' worth of w in flight per wavefront
-    __shared__ int32_t part[WAVES > 1 ? (WAVES - 1) * MT * V * 64 : 1];
+    static_assert(U <= WAVES, "less than a stretch is left: one instruction per wavefront at most");
+    __shared__ int32_t part[(WAVES - 1) * V * 64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int n0 = static_cast<int>(blockIdx.x) * BN, m0 = static_cast<int>(blockIdx.y) * (MT * BN), r = lane % BN, kq = 16 * (lane / BN);
-    const int8_t* w = a.w + static_cast<int64_t>(min(n0 + r, a.N - 1)) * a.ldw;   // (rows past the end repeat the last one: their results are not stored)
-    const int8_t* x[MT];
+    const int n0 = static_cast<int>(blockIdx.x) * BN, m0 = static_cast<int>(blockIdx.y) * BN, r = lane % BN, kq = 16 * (lane / BN);
+    const int8_t* w = a.w + static_cast<int64_t>(min(n0 + r, a.N - 1)) * a.ldw + kq;   // (rows past the end repeat the last one: their results are not stored)
+    const int8_t* x = a.x + static_cast<int64_t>(min(m0 + r, a.M - 1)) * a.ldx + kq;
+    acc_t acc;
 #pragma unroll
-    for (int t = 0; t < MT; ++t) x[t] = a.x + static_cast<int64_t>(min(m0 + t * BN + r, a.M - 1)) * a.ldx;
-    acc_t acc[MT];
+    for (int v = 0; v < V; ++v) acc[v] = 0;
+    const int K = a.K, whole = K / (KI * U), rest = whole * (KI * U) + wave * KI;
+    const i32x4 w_rest = q8_load(w, rest, K - kq, true), x_rest = q8_load(x, rest, K - kq, true);
+    i32x4 wf[2][U], xf[2][U];
+    auto load = [&](int s, int to) {
 #pragma unroll
-    for (int t = 0; t < MT; ++t)
+        for (int u = 0; u < U; ++u) __builtin_memcpy(&wf[to][u], w + s * (KI * U) + u * KI, 16);
 #pragma unroll
-        for (int v = 0; v < V; ++v) acc[t][v] = 0;
-    const int K = a.K, whole = K / (KI * U);   // stretches of KI * U
-    for (int s = wave; s < whole; s += WAVES) {
-        const int k = s * (KI * U) + kq;
-        i32x4 wf[U], xf[MT][U];
+        for (int u = 0; u < U; ++u) __builtin_memcpy(&xf[to][u], x + s * (KI * U) + u * KI, 16);
+    };
+    auto multiply = [&](int from) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) __builtin_memcpy(&wf[u], w + k + u * KI, 16);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) __builtin_memcpy(&xf[t][u], x[t] + k + u * KI, 16);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) acc[t] = q8_mma(wf[u], xf[t][u], acc[t]);
+        for (int u = 0; u < U; ++u) acc = q8_mma(wf[from][u], xf[from][u], acc);
+    };
+    if (wave < whole) load(wave, 0);
+    for (int s = wave; s < whole; s += 2 * WAVES) {
+        if (s + WAVES < whole) load(s + WAVES, 1);
+        multiply(0);
+        if (s + WAVES >= whole) break;
+        if (s + 2 * WAVES < whole) load(s + 2 * WAVES, 0);
+        multiply(1);
     }
-    for (int k = whole * (KI * U) + wave * KI; k < K; k += WAVES * KI) {   // the rest, in single instructions
-        const i32x4 wf = q8_load(w, k + kq, K, true);
+    acc = q8_mma(w_rest, x_rest, acc);
+    if (wave > 0) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) acc[t] = q8_mma(wf, q8_load(x[t], k + kq, K, true), acc[t]);
+        for (int v = 0; v < V; ++v) part[((wave - 1) * V + v) * 64 + lane] = acc[v];
     }
-    if constexpr (WAVES > 1) {
-        if (wave > 0) {
+    __syncthreads();
+    if (wave > 0) return;
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
+    for (int q = 0; q < WAVES - 1; ++q)
 #pragma unroll
-                for (int v = 0; v < V; ++v) part[((wave - 1) * MT * V + t * V + v) * 64 + lane] = acc[t][v];
-        }
-        __syncthreads();
-        if (wave > 0) return;
-#pragma unroll
-        for (int q = 0; q < WAVES - 1; ++q)
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int v = 0; v < V; ++v) acc[t][v] += part[(q * MT * V + t * V + v) * 64 + lane];
-    }
+        for (int v = 0; v < V; ++v) acc[v] += part[(q * V + v) * 64 + lane];
+    const int m = m0 + r;
+    const float sx = a.sx[min(m, a.M - 1)];
 #pragma unroll
     for (int g = 0; g < V / 4; ++g) {
         const Q8Columns c = q8_columns(a, n0 + (BN == 16 ? 4 * (lane / BN) : 8 * g + 4 * (lane / BN)));
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const int m = m0 + t * BN + r;
-            q8_store<T>(a, c, m, a.sx[min(m, a.M - 1)], acc[t][4 * g], acc[t][4 * g + 1], acc[t][4 * g + 2], acc[t][4 * g + 3]);
-        }
+        q8_store<T>(a, c, m, sx, acc[4 * g], acc[4 * g + 1], acc[4 * g + 2], acc[4 * g + 3]);
     }
 }
 
@@ -502,19 +492,20 @@ template <typename T, int TILE, int THREADS, bool ALIGNED> static int launch_til
 template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
 {
     const auto blocks = [&](int bn, int bm) { return dim3(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + bm - 1) / bm)); };
-    if (a.M <= 16) {
-        hipLaunchKernelGGL((q8_stream_kernel<T, 16, 1, 8>), blocks(16, 16), dim3(512), 0, st, a);
-        DQN_LAUNCH_CHECK();
-        return DQN_OK;
-    }
     const auto tiles = [&](int64_t t) { return (a.M + t - 1) / t * ((a.N + t - 1) / t); };
-    if (tiles(64) < 128) {
-        hipLaunchKernelGGL((q8_stream_kernel<T, 32, 1, 8>), blocks(32, 32), dim3(512), 0, st, a);
+    // Up to 16 rows of x, and where tiles of 64 would leave half of the chip idle: streamed.  A short k has four wavefronts, a longer one eight (1x65536x1024 13 us with four, 18
+    // with eight; 1x16384x4096 17 and 13); sixteen on half stretches lose (200x300x16384 45 us where eight take 31).
+    if (a.M <= 16 || tiles(64) < 128) {
+        if (a.M <= 16 && a.K < 2048) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
+        else if (a.M <= 16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 8>), blocks(16, 16), dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((q8_stream_kernel<T, 32, 8, 8>), blocks(32, 32), dim3(512), 0, st, a);
         DQN_LAUNCH_CHECK();
         return DQN_OK;
     }
     // 16-byte loads straight into LDS need rows on 16-byte borders; a lane's place within a tile is a 32-bit offset
     const bool aligned = aligned16(a.x) && aligned16(a.w) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.ldx < (1 << 23) && a.ldw < (1 << 23);
+    // The largest tile of which there are enough: a smaller one reads its operands more often, a larger one leaves compute units idle (64 / 128: 1111x2051x2003 18 / 19 us, 1024^3 6.5 / 9.8, 2048^3
+    // 19.7 / 16.6, 256x16384x4096 36 / 28; 128 / 256: 8192^3 packed, where there is no 256, 1105 us, 600 with).
     if (tiles(128) < 200) return aligned ? launch_tile<T, 64, 256, true>(a, st) : launch_tile<T, 64, 256, false>(a, st);
     if (tiles(256) < 192) return aligned ? launch_tile<T, 128, 256, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
     return aligned ? launch_tile<T, 256, 512, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
