@@ -268,9 +268,10 @@ int dqn_train_step_sampled(dqn_ctx* ctx, replay* rb, int32_t B, uint64_t sample_
  *   q_c = the whole number nearest to 127 x_c / a (the exact quotient; ties to even),
  * and, if values != NULL, values_c = q_c * scale rounded to fp32 (at most its largest number) and then to x's type: what the levels stand for.  q or values may be NULL, not both.
  * A row of zeros (or cols = 0) has scale 0 and levels 0; a row that holds a NaN or an infinity has scale NaN and levels 0, so that
- * whatever is computed from it is NaN.  Errors: DQN_EINVAL (type, sizes outside 0..4194304 rows and 0..2^31-1 columns, a pitch shorter
+ * whatever is computed from it is NaN.  Errors: DQN_EINVAL (type, sizes outside 0..4194303 rows and 0..2^30 columns, a pitch shorter
  * than a row, null / misaligned pointer). */
-#define Q8_QUANTIZE_MAX_ROWS 4194304
+#define Q8_QUANTIZE_MAX_ROWS 4194303
+#define Q8_QUANTIZE_MAX_COLS 1073741824
 int q8_quantize_rows(const void* x, int32_t type, int64_t ldx, int64_t rows, int64_t cols, int8_t* q, int64_t ldq, float* scale, void* values, int64_t ldv,
                      void* stream);
 
@@ -299,8 +300,8 @@ int q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, in
  * same on every run.
  * work: device memory of at least policy_sample_workspace(rows, n) bytes (NULL where that is 0), 16-byte aligned; it needs no
  * clearing, and two calls that may overlap in time (on two streams, or in two graphs) need one each.  Errors: DQN_EINVAL (type, rows outside
- * 0..4194304, n outside 0..4194304, ld < n, null / misaligned pointer, work too small). */
-#define POLICY_SAMPLE_MAX_ROWS 4194304
+ * 0..4194303, n outside 0..4194304, ld < n, null / misaligned pointer, work too small). */
+#define POLICY_SAMPLE_MAX_ROWS 4194303
 #define POLICY_SAMPLE_MAX_N 4194304
 size_t policy_sample_workspace(int64_t rows, int64_t n);
 int policy_sample(const void* scores, int32_t type, int64_t ld, int64_t rows, int64_t n, const float* temperature, const int32_t* top_k, const float* top_p,

@@ -22,8 +22,8 @@ DQN_OK, DQN_EINVAL, DQN_EHIP, DQN_ENOMEM, DQN_ESTATE = 0, -1, -2, -3, -4
 DQN_PRECISION_FP32, DQN_PRECISION_BF16 = 0, 1
 DQN_TYPE_FP32, DQN_TYPE_BF16, DQN_TYPE_FP16 = 0, 1, 2
 DQN_ACT_STATIC_MAX_ENVS = 32
-Q8_QUANTIZE_MAX_ROWS, Q8_LINEAR_MAX_ROWS, Q8_LINEAR_MAX_K = 4194304, 524288, 131071
-POLICY_SAMPLE_MAX_ROWS = POLICY_SAMPLE_MAX_N = 4194304
+Q8_QUANTIZE_MAX_ROWS, Q8_QUANTIZE_MAX_COLS, Q8_LINEAR_MAX_ROWS, Q8_LINEAR_MAX_K = 4194303, 1 << 30, 524288, 131071
+POLICY_SAMPLE_MAX_ROWS, POLICY_SAMPLE_MAX_N = 4194303, 4194304
 DQN_PARAMS_ONLINE, DQN_PARAMS_TARGET, DQN_PARAMS_RMS_V, DQN_PARAMS_RMS_M, DQN_PARAMS_GRAD = range(5)
 
 

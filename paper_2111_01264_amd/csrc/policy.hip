@@ -670,6 +670,7 @@ __device__ __forceinline__ void draw(RowShared<THREADS>& sh, const PolicyArgs& a
         if (owner < 0 && target < sh.mass[q]) owner = q;
         if (owner < 0) target -= sh.mass[q];
     }
+    if (owner < 0) return;   // (not reached: the kept sums of a stretch are the same whole numbers wherever they are taken)
     // the stretch of that group, shared out among all threads
     const int begin = ((owner >> 2) * row.trips + (owner & 3) * per) * 64 * E, end = min(row.n, ((owner >> 2) * row.trips + min(((owner & 3) + 1) * per, row.trips)) * 64 * E);
     const int each = (end - begin + THREADS - 1) / THREADS, from = begin + t * each, to = min(end, from + each);

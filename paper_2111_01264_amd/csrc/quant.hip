@@ -529,7 +529,7 @@ int q8_quantize_rows(const void* x, int32_t type, int64_t ldx, int64_t rows, int
 {
     const char* who = "q8_quantize_rows";
     if (int rc = check_type(who, type)) return rc;
-    if (rows < 0 || rows > Q8_QUANTIZE_MAX_ROWS || cols < 0 || cols > INT32_MAX) return fail(DQN_EINVAL, "%s: rows = %lld, cols = %lld", who, (long long)rows, (long long)cols);
+    if (rows < 0 || rows > Q8_QUANTIZE_MAX_ROWS || cols < 0 || cols > Q8_QUANTIZE_MAX_COLS) return fail(DQN_EINVAL, "%s: rows = %lld, cols = %lld", who, (long long)rows, (long long)cols);
     if (rows == 0) return DQN_OK;
     if (!scale || (cols && (!x || (!q && !values)))) return fail(DQN_EINVAL, "%s: null pointer", who);
     const uintptr_t e = type == DQN_TYPE_FP32 ? 4 : 2;

@@ -20,7 +20,7 @@ QUANT_GOOD = dict(x=A, type=1, ldx=8, rows=2, cols=8, q=A, ldq=8, scale=A, value
 
 
 def test_quantize_refusals():
-    for bad in (dict(type=3), dict(type=-1), dict(rows=-1), dict(cols=-1), dict(rows=P.Q8_QUANTIZE_MAX_ROWS + 1), dict(cols=1 << 31), dict(x=None), dict(scale=None),
+    for bad in (dict(type=3), dict(type=-1), dict(rows=-1), dict(cols=-1), dict(rows=P.Q8_QUANTIZE_MAX_ROWS + 1), dict(cols=P.Q8_QUANTIZE_MAX_COLS + 1, ldx=1 << 31, ldq=1 << 31), dict(x=None), dict(scale=None),
                 dict(q=None), dict(ldx=7), dict(ldq=7), dict(values=A, ldv=7), dict(x=A + 1), dict(type=0, x=A + 2), dict(scale=A + 2), dict(values=A + 1, ldv=8)):
         assert call("q8_quantize_rows", QUANT, QUANT_GOOD, **bad) == P.DQN_EINVAL, bad
         assert b"q8_quantize_rows" in LIB.dqn_last_error()

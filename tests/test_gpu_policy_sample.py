@@ -99,6 +99,39 @@ def test_many_rows(rows, n):
     Call(x, n, torch.rand(rows, generator=g, device="cuda"), pick([0.0, 0.5, 1.0, 3.0]), pick([0, 1, 2, 7, n]), pick([0.5, 0.9, 1.0]), pick([0.0, 0.1])).run()
 
 
+@pytest.mark.parametrize("kind", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,n", [(9, 49151), (9, 49152), (70, 50000), (128, 49999), (130, 49999), (2, 300000)])
+def test_rows_shared_out_and_not(kind, rows, n):
+    """Both sides of the lines between one workgroup per row and several, filters mixed."""
+    g = gen(rows * n)
+    x = (2 * torch.randn(rows, n, generator=g, device="cuda")).to(TYPES[kind][0])
+    x[1::3, ::7] = -INF
+    pick = lambda v: torch.tensor(v, device="cuda")[torch.randint(len(v), (rows,), generator=g, device="cuda")]  # noqa: E731
+    u = torch.rand(rows, generator=g, device="cuda")
+    Call(x, n, u, pick([0.0, 0.7, 1.0, 1.0, 4.0]), pick([0, 0, 30, 192, 193, 5000, n // 2]), pick([0.3, 0.9, 0.99, 1.0]), pick([0.0, 0.0, 0.01])).run()
+    Call(x, n, u, p=pick([0.5, 0.95])).run()
+    Call(x, n, u, t=pick([0.5, 2.0])).run()
+
+
+@pytest.mark.parametrize("n", [17000, 60000])
+def test_bf16_values_of_every_size(n):
+    """Zeros, tiny, ordinary and large values, of few and of many kinds: those that have a place in the table of values and those that have none."""
+    g = gen(n)
+    rows = 140
+    x = 2 * torch.randn(rows, n, generator=g, device="cuda")
+    x[0::7, ::3] = 0.0
+    x[1::7, ::2] *= 1e-9
+    x[2::7, ::5] = -400.0
+    x[3::7] = torch.round(x[3::7])
+    x[4::7] *= 2.0 ** -30
+    x[5::7, 5] = 3e4
+    x = x.bfloat16()
+    u = torch.rand(rows, generator=g, device="cuda")
+    rep = lambda v: torch.tensor([v[(r // 7) % len(v)] for r in range(rows)])  # noqa: E731
+    Call(x, n, u, rep([1.0, 0.5, 30.0, 1.0]), rep([0, 300, 0, 2000, 40]), rep([0.9, 1.0, 0.5, 0.99])).run()
+    Call(x, n, u, rep([1.0, 200.0]), None, None, rep([0.0, 0.001])).run()
+
+
 @pytest.mark.parametrize("n", [6, 40, 700, 5000, 40000])
 def test_equal_scores_go_by_index(n):
     """Weights of exactly 1: kept sets and borders are whole numbers, with no rounding anywhere."""

@@ -102,7 +102,7 @@ def test_scales_at_the_ends_and_nan():
 
 
 def test_no_levels_leave_the_bias():
-    for M, N in ((2, 37), (300, 70)):
+    for M, N in ((2, 37), (300, 70), (1500, 1200), (4000, 3900)):
         b = torch.randn(N, device="cuda")
         y = torch.zeros(M, N, device="cuda")
         s = torch.ones(max(M, N), device="cuda")
