@@ -139,20 +139,18 @@ def _ptr(t):
     return t.data_ptr()
 
 
-_TYPES = (torch.float32, torch.bfloat16, torch.float16)   # by DQN_TYPE_*
+_TYPES = {DQN_TYPE_FP32: torch.float32, DQN_TYPE_BF16: torch.bfloat16, DQN_TYPE_FP16: torch.float16}
+_F32, _I32, _I8 = torch.float32, torch.int32, torch.int8
 
 
 def _rows(t, dtype):
-    """Matrix of the given element type whose rows are contiguous (its pitch is an argument of its own) -> address, None -> NULL."""
+    """Matrix of the given element type whose rows are contiguous (its pitch is an argument of its own) -> address, None -> NULL.
+    An unknown DQN_TYPE_* (dtype None) is left to the library to refuse."""
     if t is None:
         return None
-    assert t.dtype is dtype and (t.is_contiguous() or t.stride(-1) == 1), \
-        "a matrix handed to the library has another element type, or rows that are not contiguous"
+    assert t.dtype is dtype or dtype is None, "a matrix handed to the library has another element type"
+    assert t.is_contiguous() or t.stride(-1) == 1, "rows of a matrix handed to the library must be contiguous"
     return t.data_ptr()
-
-
-def _typed(t, type):
-    return _rows(t, _TYPES[type]) if 0 <= type < len(_TYPES) else _rows(t, None if t is None else t.dtype)
 
 
 def _vec(t, dtype):
@@ -211,10 +209,9 @@ def dqn_act_static(ctx, states, W, epsilon, act_step, use_target, actions, q_out
 
 def dqn_act_sampled(ctx, states, W, temperature, top_k, top_p, min_p, u, act_step, use_target, quantized, actions, q_out=None,
                     logp=None):
-    f32 = torch.float32
-    _check(_lib.dqn_act_sampled(ctx, _ptr(states), W, _vec(temperature, f32), _vec(top_k, torch.int32), _vec(top_p, f32),
-                                _vec(min_p, f32), _vec(u, f32), act_step, use_target, quantized, _vec(actions, torch.int32),
-                                _vec(q_out, f32), _vec(logp, f32)))
+    _check(_lib.dqn_act_sampled(ctx, _ptr(states), W, _vec(temperature, _F32), _vec(top_k, _I32), _vec(top_p, _F32),
+                                _vec(min_p, _F32), _vec(u, _F32), act_step, use_target, quantized, _vec(actions, _I32),
+                                _vec(q_out, _F32), _vec(logp, _F32)))
 
 
 def dqn_quantize_actor(ctx, use_target):
@@ -282,13 +279,18 @@ def replay_sample_gather(rb, B, sample_step, idx_in, s, s2, a, r, done, idx_out=
 
 
 def q8_quantize_rows(x, type, ldx, rows, cols, q, ldq, scale, values, ldv, stream):
-    _check(_lib.q8_quantize_rows(_typed(x, type), type, ldx, rows, cols, _rows(q, torch.int8), ldq, _vec(scale, torch.float32),
-                                 _typed(values, type), ldv, _stream(stream)))
+    dtype = _TYPES.get(type)
+    rc = _lib.q8_quantize_rows(_rows(x, dtype), type, ldx, rows, cols, _rows(q, _I8), ldq, _vec(scale, _F32),
+                               _rows(values, dtype), ldv, None if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def q8_linear(x, ldx, sx, w, ldw, sw, bias, relu, M, N, K, y, type, ldy, stream):
-    _check(_lib.q8_linear(_rows(x, torch.int8), ldx, _vec(sx, torch.float32), _rows(w, torch.int8), ldw, _vec(sw, torch.float32),
-                          _vec(bias, torch.float32), relu, M, N, K, _typed(y, type), type, ldy, _stream(stream)))
+    rc = _lib.q8_linear(_rows(x, _I8), ldx, _vec(sx, _F32), _rows(w, _I8), ldw, _vec(sw, _F32), _vec(bias, _F32), relu,
+                        M, N, K, _rows(y, _TYPES.get(type)), type, ldy, None if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def policy_sample_workspace(rows, n):
@@ -296,10 +298,12 @@ def policy_sample_workspace(rows, n):
 
 
 def policy_sample(scores, type, ld, rows, n, temperature, top_k, top_p, min_p, u, index, logp, work, work_bytes, stream):
-    f32 = torch.float32
-    _check(_lib.policy_sample(_typed(scores, type), type, ld, rows, n, _vec(temperature, f32), _vec(top_k, torch.int32),
-                              _vec(top_p, f32), _vec(min_p, f32), _vec(u, f32), _vec(index, torch.int32), _vec(logp, f32),
-                              _ptr(work), work_bytes, _stream(stream)))
+    rc = _lib.policy_sample(_rows(scores, _TYPES.get(type)), type, ld, rows, n, _vec(temperature, _F32), _vec(top_k, _I32),
+                            _vec(top_p, _F32), _vec(min_p, _F32), _vec(u, _F32), _vec(index, _I32), _vec(logp, _F32),
+                            None if work is None else work.data_ptr(), work_bytes,
+                            None if stream is None else stream.cuda_stream)
+    if rc:
+        _check(rc)
 
 
 def synth_frames(dst, n, id0, id_step, seed, stream_tag, pix_threshold, background, stream):
