@@ -637,23 +637,30 @@ __device__ __forceinline__ void draw(RowShared<THREADS>& sh, const PolicyArgs& a
             left = per;
             ++group;
         };
-        row.template each<1>([&](int first, const typename ROW::vec& v) {
-            if (!ROW::any(v, kept.score)) {
-            } else if (table) {
+        if (table) {
+            row.template each<4>([&](int first, const typename ROW::vec& v) {
+                if (ROW::any(v, kept.score)) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float x = static_cast<float>(v[e]);
-                    if (x > kept.score || (x == kept.score && first + e <= kept.index)) {
-                        const uint32_t place = table_place(v[e]);
-                        sum += place < kTablePlaces ? reinterpret_cast<const double*>(table)[place] : kept(w, x, first + e);
+                    for (int e = 0; e < E; ++e) {
+                        const float x = static_cast<float>(v[e]);
+                        if (x > kept.score || (x == kept.score && first + e <= kept.index)) {
+                            const uint32_t place = table_place(v[e]);
+                            if (place < kTablePlaces) sum += reinterpret_cast<const double*>(table)[place];
+                            else if (x > -INFINITY) sum += kept(w, x, first + e);
+                        }
                     }
                 }
-            } else {
+                if (--left == 0) close();
+            });
+        } else {
+            row.template each<1>([&](int first, const typename ROW::vec& v) {
+                if (ROW::any(v, kept.score)) {
 #pragma unroll
-                for (int e = 0; e < E; ++e) sum += kept(w, static_cast<float>(v[e]), first + e);
-            }
-            if (--left == 0) close();
-        });
+                    for (int e = 0; e < E; ++e) sum += kept(w, static_cast<float>(v[e]), first + e);
+                }
+                if (--left == 0) close();
+            });
+        }
         if (left < per) close();
     }
 #pragma unroll
