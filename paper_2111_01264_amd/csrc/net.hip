@@ -129,8 +129,8 @@ struct dqn_ctx {
     int last_B = 0;
     int num_cus = 256;
     // the quantised actor (dqn_quantize_actor): levels and scales of fc1.w [512][3136] and fc2.w [A][512] (device layout), and the act step's intermediates
-    int8_t *q8_w1 = nullptr, *q8_w2 = nullptr, *q8_x = nullptr, *q8_h = nullptr;
-    float *q8_s1 = nullptr, *q8_s2 = nullptr, *q8_sx = nullptr, *q8_sh = nullptr, *q8_hidden = nullptr;
+    int8_t *q8_w1 = nullptr, *q8_w2 = nullptr, *q8_x = nullptr;
+    float *q8_s1 = nullptr, *q8_s2 = nullptr, *q8_sx = nullptr, *q8_hidden = nullptr;
     // theta (0) and theta^- (1) change: how often they have, and at which count the levels were made (0: never).  Those of theta are read and written under online_mu.
     std::atomic<uint64_t> changes[2] = {{1}, {1}};
     uint64_t q8_at[2] = {0, 0};
@@ -389,9 +389,9 @@ static int act_impl(dqn_ctx* c, Workspace& ws, const uint8_t* states, int W, flo
     return DQN_OK;
 }
 
-// Q rows [W][A] of the quantised actor: the conv layers as ever, then fc1 and fc2 on 8-bit levels, each input row quantised with a scale of its own.
+// The quantised actor's Q rows [W][A] and the draw from them: the conv layers as ever, then fc1 and fc2 on 8-bit levels, each input row quantised with a scale of its own.
 template <typename T>
-static int q8_rows(dqn_ctx* c, const uint8_t* states, int W, int use_target, float* q)
+static int q8_act(dqn_ctx* c, const uint8_t* states, int W, int use_target, float* q, const PolicyArgs& policy)
 {
     const Offsets& o = c->off;
     hipStream_t st = c->act_stream;
@@ -405,9 +405,7 @@ static int q8_rows(dqn_ctx* c, const uint8_t* states, int W, int use_target, flo
     if (rc != DQN_OK) return rc;
     rc = enqueue_q8_linear(c->q8_x, 3136, c->q8_sx, c->q8_w1, 3136, c->q8_s1, master[0] + o.bf1, true, W, 512, 3136, c->q8_hidden, DQN_TYPE_FP32, 512, st);
     if (rc != DQN_OK) return rc;
-    rc = enqueue_quantize_rows(c->q8_hidden, DQN_TYPE_FP32, 512, W, 512, c->q8_h, 512, c->q8_sh, nullptr, 0, st);
-    if (rc != DQN_OK) return rc;
-    return enqueue_q8_linear(c->q8_h, 512, c->q8_sh, c->q8_w2, 512, c->q8_s2, master[0] + o.bf2, false, W, c->A, 512, q, DQN_TYPE_FP32, c->A, st);
+    return enqueue_policy_q8_head(policy, c->q8_hidden, c->q8_w2, c->q8_s2, master[0] + o.bf2, q, W, st);
 }
 
 template <typename T>
@@ -717,11 +715,9 @@ int dqn_create(const dqn_config* cfg, void* act_stream, void* train_stream, dqn_
         DQN_HIP(hipMalloc((void**)&c->q8_w1, 512 * 3136));
         DQN_HIP(hipMalloc((void**)&c->q8_w2, A * 512));
         DQN_HIP(hipMalloc((void**)&c->q8_x, E * 3136));
-        DQN_HIP(hipMalloc((void**)&c->q8_h, E * 512));
         DQN_HIP(hipMalloc((void**)&c->q8_s1, 512 * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->q8_s2, A * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->q8_sx, E * sizeof(float)));
-        DQN_HIP(hipMalloc((void**)&c->q8_sh, E * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->q8_hidden, E * 512 * sizeof(float)));
         for (int i = 0; i < 2; ++i) {
             DQN_HIP(hipMalloc((void**)&c->mb_s[i], B * kStateBytes));
@@ -760,8 +756,8 @@ int dqn_destroy(dqn_ctx* c)
     (void)hipFree(c->dzh); (void)hipFree(c->dz3); (void)hipFree(c->dz2); (void)hipFree(c->dz1);
     (void)hipFree(c->dqv); (void)hipFree(c->lossv); (void)hipFree(c->loss_keep);
     (void)hipFree(c->bsh); (void)hipFree(c->bias_partial); (void)hipFree(c->wg_partial);
-    (void)hipFree(c->q8_w1); (void)hipFree(c->q8_w2); (void)hipFree(c->q8_x); (void)hipFree(c->q8_h); (void)hipFree(c->q8_s1); (void)hipFree(c->q8_s2);
-    (void)hipFree(c->q8_sx); (void)hipFree(c->q8_sh); (void)hipFree(c->q8_hidden);
+    (void)hipFree(c->q8_w1); (void)hipFree(c->q8_w2); (void)hipFree(c->q8_x); (void)hipFree(c->q8_s1); (void)hipFree(c->q8_s2);
+    (void)hipFree(c->q8_sx); (void)hipFree(c->q8_hidden);
     for (int i = 0; i < 2; ++i) {
         (void)hipFree(c->mb_s[i]); (void)hipFree(c->mb_s2[i]); (void)hipFree(c->mb_a[i]); (void)hipFree(c->mb_r[i]); (void)hipFree(c->mb_d[i]);
         (void)hipFree(c->mb_desc[i]);
@@ -940,13 +936,17 @@ int dqn_act_sampled(dqn_ctx* c, const uint8_t* states, int32_t W, const float* t
     if (!use_target) DQN_HIP(wait_for_train(c));
     float* q = q_out ? q_out : c->act_ws.q;
     const bool bf16 = c->cfg.precision == DQN_PRECISION_BF16;
-    int rc;
-    if (quantized) rc = bf16 ? q8_rows<bf16_t>(c, states, W, use_target, q) : q8_rows<float>(c, states, W, use_target, q);
-    else rc = bf16 ? act_impl<bf16_t>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q) : act_impl<float>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q);
-    if (rc != DQN_OK) return rc;
     const PolicyArgs pa{q, c->A, c->A, temperature, top_k, top_p, min_p, u, c->cfg.seed, act_step, actions, logp};
-    rc = enqueue_policy_sample(pa, DQN_TYPE_FP32, W, nullptr, c->act_stream);   // (rows this short need no workspace)
-    if (rc != DQN_OK) return rc;
+    int rc;
+    if (quantized) {
+        rc = bf16 ? q8_act<bf16_t>(c, states, W, use_target, q, pa) : q8_act<float>(c, states, W, use_target, q, pa);
+        if (rc != DQN_OK) return rc;
+    } else {
+        rc = bf16 ? act_impl<bf16_t>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q) : act_impl<float>(c, c->act_ws, states, W, 0.f, act_step, use_target, actions, q);
+        if (rc != DQN_OK) return rc;
+        rc = enqueue_policy_sample(pa, DQN_TYPE_FP32, W, nullptr, c->act_stream);   // (rows this short need no workspace)
+        if (rc != DQN_OK) return rc;
+    }
     if (!use_target) {
         DQN_HIP(hipEventRecord(c->ev_act, c->act_stream));
         c->act_reads_online.store(true, std::memory_order_release);

@@ -2,6 +2,7 @@
 #include <type_traits>
 
 #include "policy.h"
+#include "quant.h"
 
 #include "gemm_mfma.h"
 
@@ -117,14 +118,10 @@ __device__ inline uint64_t wave_scan(uint64_t v)   // inclusive
 // ---- short rows: a wavefront each, a lane for each score -------------------------------------------------------------------------
 //
 // What lies before an entry in the filters' order is counted and summed against all n others (n <= 64), so nothing is sorted.
-template <typename T>
-__global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t rows)
+__device__ __forceinline__ void short_row(const PolicyArgs& a, int64_t row, float x)   // x: this lane's score, -infinity where there is none
 {
     const int lane = threadIdx.x & 63;
-    const int64_t row = blockIdx.x * 4ll + (threadIdx.x >> 6);
-    if (row >= rows) return;
     const RowSettings s = row_settings(a, row);
-    const float x = lane < a.n ? static_cast<float>(static_cast<const T*>(a.scores)[row * a.ld + lane]) : -INFINITY;
     const bool nan = __any(x != x);
     float m = x;
     for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
@@ -160,6 +157,58 @@ __global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t
     const uint64_t target = static_cast<uint64_t>(s.u * static_cast<double>(total));
     const int pick = __builtin_ctzll(__ballot(sum > target));   // (total is at least 2^40 and u is below 1)
     if (lane == pick) answer(a, row, pick, log_probability(x, w, s.t, total));
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t rows)
+{
+    const int lane = threadIdx.x & 63;
+    const int64_t row = blockIdx.x * 4ll + (threadIdx.x >> 6);
+    if (row >= rows) return;
+    short_row(a, row, lane < a.n ? static_cast<float>(static_cast<const T*>(a.scores)[row * a.ld + lane]) : -INFINITY);
+}
+
+// A workgroup per row: two hidden values per thread become levels in LDS, eight threads sum the products of one action, the first wavefront draws.  Nothing but the chain of launches bounds
+// a call this small, and this is one instead of three (act step of 8 states, bf16: HEAD_US).
+__global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q)
+{
+    __shared__ uint32_t part[4];
+    __shared__ alignas(16) int8_t levels[512];
+    __shared__ float scores[32];
+    const int64_t row = blockIdx.x;
+    const int t = threadIdx.x;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    const f32x2 h = reinterpret_cast<const f32x2*>(hidden + row * 512)[t];
+    uint32_t top = max(magnitude(h[0]), magnitude(h[1]));
+    for (int d = 32; d; d >>= 1) top = max(top, static_cast<uint32_t>(__shfl_xor(static_cast<int>(top), d)));
+    if ((t & 63) == 0) part[t >> 6] = top;
+    __syncthreads();
+    top = max(max(part[0], part[1]), max(part[2], part[3]));
+    const bool finite = top < 0x7F800000u;
+    const float m = finite ? __uint_as_float(top) : 0.f, s = finite ? row_scale(m) : not_a_number();
+    const Levels l = make_levels(m);
+    levels[2 * t] = static_cast<int8_t>(finite ? level_of(l, h[0]) : 0);
+    levels[2 * t + 1] = static_cast<int8_t>(finite ? level_of(l, h[1]) : 0);
+    __syncthreads();
+    const int action = t >> 3, k = (t & 7) * 64;
+    int32_t acc = 0;
+    if (action < a.n) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const i32x4 v = *reinterpret_cast<const i32x4*>(w + action * 512 + k + 16 * i), x = *reinterpret_cast<const i32x4*>(levels + k + 16 * i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_sdot4(v[e], x[e], acc, false);
+        }
+    }
+    for (int d = 4; d; d >>= 1) acc += __shfl_xor(acc, d);
+    if ((t & 7) == 0 && action < a.n) {
+        const float v = q8_result<float>(acc, s, scales[action], bias[action], -INFINITY);
+        scores[action] = v;
+        q[row * a.n + action] = v;
+    }
+    __syncthreads();
+    if (t < 64) short_row(a, row, t < a.n ? scores[t] : -INFINITY);
 }
 
 // ---- longer rows: what the kernels below share ------------------------------------------------------------------------------
@@ -1039,6 +1088,13 @@ template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows
         if (smem) DQN_HIP(raise_dynamic_lds(reinterpret_cast<const void*>(policy_row_kernel<T, 1024>), smem));
         hipLaunchKernelGGL((policy_row_kernel<T, 1024>), grid, dim3(1024), smem, st, a);
     }
+    DQN_LAUNCH_CHECK();
+    return DQN_OK;
+}
+
+int enqueue_policy_q8_head(const PolicyArgs& a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q, int64_t rows, hipStream_t st)
+{
+    hipLaunchKernelGGL(policy_q8_head_kernel, dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, hidden, w, scales, bias, q);
     DQN_LAUNCH_CHECK();
     return DQN_OK;
 }

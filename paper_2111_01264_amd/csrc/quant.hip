@@ -9,37 +9,6 @@ namespace dqn {
 
 // ---- rows to levels -------------------------------------------------------------------------------------------------
 //
-// scale = fl(a / 127), level = rint(127 x / a) with a = max |x| of the row.  The level is rint of the EXACT quotient: the fp32 quotient
-// is off by less than 2^-15 of a level, so only a value that close to the border between two levels is decided again, in fp64, where
-// 127 x - level a has no rounding.
-__device__ inline float row_scale(float a) { return static_cast<float>(static_cast<double>(a) / 127.0); }
-
-struct Levels {
-    float a, inv;   // the row's largest magnitude and 127 / a, both times `up`
-    float up;       // 2^64 where a is so small that 127 / a would overflow, else 1
-};
-__device__ inline Levels make_levels(float a)
-{
-    Levels l;
-    l.up = a < 0x1p-100f ? 0x1p64f : 1.f;
-    l.a = a * l.up;
-    l.inv = a > 0.f ? 127.f / l.a : 0.f;
-    return l;
-}
-__device__ inline int level_of(const Levels& l, float x)
-{
-    x *= l.up;
-    const float f = x * l.inv;
-    float q = rintf(f);
-    if (fabsf(fabsf(f - q) - 0.5f) < 0x1p-13f) {
-        const double a = l.a, r = 127.0 * x - static_cast<double>(q) * a;   // exact
-        const bool odd = static_cast<int>(q) & 1;
-        if (2.0 * r > a || (2.0 * r == a && odd)) q += 1.f;
-        else if (2.0 * r < -a || (2.0 * r == -a && odd)) q -= 1.f;
-    }
-    return static_cast<int>(q);
-}
-
 // What a level stands for.  127 times a scale that was rounded up can lie beyond the largest fp32 number: the row's own maximum does not.
 __device__ inline float level_value(int q, float s)
 {
@@ -54,8 +23,6 @@ template <typename T> struct Vec16 {   // 16 bytes of a row, at any alignment th
 };
 
 struct QuantArgs { const void* x; int8_t* q; float* scale; void* values; int64_t ldx, ldq, ldv; int64_t rows; int cols; };
-
-template <typename T> __device__ inline uint32_t magnitude(T v) { return __float_as_uint(fabsf(static_cast<float>(v))); }   // they order as the values do, infinities and NaN above all others
 
 // Memory bounds it, so a row is read once: TPR threads hold it, R vectors of 16 bytes each, find its largest magnitude and write the levels.
 // A row beyond TPR * R vectors (R = 0) is read twice, the second time from cache.  8192x8192 bf16 with values: 64 us, 5.3 TB/s, as fast as a copy (read twice, in single
@@ -177,14 +144,6 @@ struct Q8Args {
     int64_t ldx, ldw, ldy;
     int M, N, K, relu;
 };
-
-// The sum is exact in 32-bit integers; scales and bias are applied in fp64 (their product neither overflows nor underflows there, and
-// only the result is rounded) and the result is rounded to fp32 and to y's type.  floor: 0 with a ReLU, else -infinity; a NaN stays.
-template <typename T> __device__ inline T q8_result(int32_t acc, float sx, float sw, float b, float floor)
-{
-    const float v = static_cast<float>(static_cast<double>(acc) * (static_cast<double>(sx) * static_cast<double>(sw)) + static_cast<double>(b));
-    return static_cast<T>(v < floor ? floor : v);
-}
 
 // 16 levels of a row from column k on; zeros from column K on and for rows that there are none of.
 __device__ inline i32x4 q8_load(const int8_t* row, int k, int K, bool in)
@@ -501,8 +460,9 @@ template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
     // Up to 16 rows of x, and where tiles of 64 would leave half of the chip idle: streamed.  A short k has four wavefronts, a longer one eight (1x65536x1024 13 us with four, 18
     // with eight; 1x16384x4096 17 and 13); sixteen on half stretches lose (200x300x16384 45 us where eight take 31).
     if (a.M <= 16 || tiles(64) < 128) {
-        if (a.M <= 16 && a.K < 2048) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
-        else if (a.M <= 16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 8>), blocks(16, 16), dim3(512), 0, st, a);
+        const bool by_16 = a.M <= 16 || tiles(32) < 192;
+        if (by_16 && a.K < 2048) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
+        else if (by_16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 8>), blocks(16, 16), dim3(512), 0, st, a);
         else hipLaunchKernelGGL((q8_stream_kernel<T, 32, 8, 8>), blocks(32, 32), dim3(512), 0, st, a);
         DQN_LAUNCH_CHECK();
         return DQN_OK;
