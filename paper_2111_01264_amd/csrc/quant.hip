@@ -205,7 +205,7 @@ template <typename T> __device__ inline void q8_store(const Q8Args& a, const Q8C
 
 // ---- few rows: the weights are streamed once, from memory straight into the matrix instructions ---------------------------------
 //
-// A workgroup owns BN rows of w and BN rows of x (BN = 16: all that there are; 32: a tile of them); its wavefronts take every WAVES-th stretch of k
+// A workgroup owns BN rows of w and BN rows of x; its wavefronts take every WAVES-th stretch of k
 // and meet in LDS at the end.  No staging: a row of w is used by one wavefront only, and the rows of x come from cache.  Memory's latency bounds it, so a
 // stretch's U loads of either side are requested while the one before is multiplied, and what is left behind the last stretch before anything else.
 // 1x16384x4096: 13.0 us, 5.2 TB/s; 512x512x3136: 7.9 us (each stretch's loads behind the last stretch's products: 9.4); 8x512x3136: 5.6 us, as long as any call.
@@ -457,8 +457,9 @@ template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
 {
     const auto blocks = [&](int bn, int bm) { return dim3(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + bm - 1) / bm)); };
     const auto tiles = [&](int64_t t) { return (a.M + t - 1) / t * ((a.N + t - 1) / t); };
-    // Up to 16 rows of x, and where tiles of 64 would leave half of the chip idle: streamed.  A short k has four wavefronts, a longer one eight (1x65536x1024 13 us with four, 18
-    // with eight; 1x16384x4096 17 and 13); sixteen on half stretches lose (200x300x16384 45 us where eight take 31).
+    // Up to 16 rows of x, and where tiles of 64 would leave half of the chip idle: streamed, in tiles of 16 while there are few of 32 (16 / 32: 128x512x3136 4.8 / 7.0 us, 200x300x16384
+    // 17 / 31; 384x512x3136 9.0 / 6.9, 512x512x3136 9.9 / 7.1).  A short k has four wavefronts, a longer one eight (1x65536x1024 13 us with four, 18
+    // with eight; 1x16384x4096 17 and 13).
     if (a.M <= 16 || tiles(64) < 128) {
         const bool by_16 = a.M <= 16 || tiles(32) < 192;
         if (by_16 && a.K < 2048) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
