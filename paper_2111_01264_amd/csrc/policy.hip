@@ -273,15 +273,17 @@ template <typename T, int THREADS> struct Row {
                 f(first(i), v);
             }
         } else {
+            int i = 0;
 #pragma unroll 1
-            for (int i = 0; i < trips; i += AHEAD) {
+            for (; i + AHEAD <= trips; i += AHEAD) {
                 vec v[AHEAD];
 #pragma unroll
-                for (int q = 0; q < AHEAD; ++q) v[q] = load(i + q);   // (behind the last trip: the next wavefront's scores, or -infinity; not used)
+                for (int q = 0; q < AHEAD; ++q) v[q] = load(i + q);
 #pragma unroll
-                for (int q = 0; q < AHEAD; ++q)
-                    if (i + q < trips) f(first(i + q), v[q]);
+                for (int q = 0; q < AHEAD; ++q) f(first(i + q), v[q]);
             }
+#pragma unroll 1
+            for (; i < trips; ++i) f(first(i), load(i));
         }
     }
     static __device__ __forceinline__ bool any(vec v, float bound)   // of the wavefront's scores is as large

@@ -145,11 +145,11 @@ struct Q8Args {
     int M, N, K, relu;
 };
 
-// 16 levels of a row from column k on; zeros from column K on and for rows that there are none of.
-__device__ inline i32x4 q8_load(const int8_t* row, int k, int K, bool in)
+// 16 levels of a row from column k on; zeros from column K on.
+__device__ inline i32x4 q8_load(const int8_t* row, int k, int K)
 {
     i32x4 v = {0, 0, 0, 0};
-    if (!in || k >= K) return v;
+    if (k >= K) return v;
     if (k + 16 <= K) {
         __builtin_memcpy(&v, row + k, 16);
         return v;
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(WAVES * 64) void q8_stream_kernel(Q8Args a)
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = 0;
     const int K = a.K, whole = K / (KI * U), rest = whole * (KI * U) + wave * KI;
-    const i32x4 w_rest = q8_load(w, rest, K - kq, true), x_rest = q8_load(x, rest, K - kq, true);
+    const i32x4 w_rest = q8_load(w, rest, K - kq), x_rest = q8_load(x, rest, K - kq);
     i32x4 wf[2][U], xf[2][U];
     auto load = [&](int s, int to) {
 #pragma unroll
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(THREADS, TILE == 256 ? THREADS / 256 : TILE == 128 
             for (int j = 0; j < L; ++j) __builtin_memcpy(&reg[j], ptr[j] + k, 16);
         } else {
 #pragma unroll
-            for (int j = 0; j < L; ++j) reg[j] = q8_load(ptr[j], k, K, true);
+            for (int j = 0; j < L; ++j) reg[j] = q8_load(ptr[j], k, K);
         }
     };
     auto put = [&](int step) {
@@ -422,7 +422,7 @@ __global__ __launch_bounds__(THREADS, TILE == 256 ? THREADS / 256 : TILE == 128 
 #pragma unroll
             for (int j = 0; j < L; ++j) {
                 const int8_t* p = (j < L / 2 ? wb + static_cast<int64_t>(row_of(j)) * a.ldw : xb + static_cast<int64_t>(row_of(j)) * a.ldx);
-                *reinterpret_cast<i32x4*>(q8_smem + j * (16 * THREADS) + tid * 16) = q8_load(p, k + 16 * chunk, K, true);
+                *reinterpret_cast<i32x4*>(q8_smem + j * (16 * THREADS) + tid * 16) = q8_load(p, k + 16 * chunk, K);
             }
             __syncthreads();
             read(0, 0); read(0, 1);
