@@ -138,14 +138,15 @@ int dqn_act_static(dqn_ctx* ctx, const uint8_t* states, int32_t W, float epsilon
  *   quantized != 0: fc1 and fc2 run on 8-bit levels (q8_quantize_rows and q8_linear below): weights as dqn_quantize_actor left them, a scale for each output channel; each
  *   state's features and hidden row quantised with a scale of their own; conv layers and biases as ever.
  * states, W, act_step, use_target, actions, q_out as in dqn_act, the waits for use_target = 0 among it.  Errors: DQN_EINVAL as there; DQN_ESTATE if quantized and dqn_quantize_actor
- * has not run for these parameters since they last changed (dqn_set_params; use_target: dqn_sync_target, else a train step).  In a captured graph that is checked when it is captured only:
- * a program that replays it calls dqn_quantize_actor again after every change. */
+ * has not been called for these parameters since the last call that changes them (dqn_set_params; use_target: dqn_sync_target, else a train step).  For that a call that is captured
+ * into a graph counts when it is captured.  What graphs make of it when they run (or do not) is checked on the device: where the levels are not those of the parameters as they are
+ * then, all actions are -1 and all Q values and logp NaN.  A program that replays such a graph calls dqn_quantize_actor after every change, or captures it too. */
 int dqn_act_sampled(dqn_ctx* ctx, const uint8_t* states, int32_t W, const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
                     const float* u, uint64_t act_step, int32_t use_target, int32_t quantized, int32_t* actions, float* q_out, float* logp);
 
 /* Makes the 8-bit levels of fc1.w and fc2.w of theta^- (use_target != 0) or theta for dqn_act_sampled, on act_stream (theta: behind the last enqueued train step, as dqn_act).  The
  * parameters that act under Concurrent Training are constant between synchronisation points (Section 3), so once after each dqn_sync_target is enough.  A context holds
- * the levels of one network at a time.  Must not be called concurrently with dqn_act_sampled on the same ctx. */
+ * the levels of one network at a time.  Must not be called concurrently with itself or dqn_act_sampled on the same ctx. */
 int dqn_quantize_actor(dqn_ctx* ctx, int32_t use_target);
 
 /* ---- minibatch train step (Section 2.1, Eq. 1; Appendix B) -------------------------------- */

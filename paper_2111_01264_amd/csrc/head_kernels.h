@@ -558,6 +558,7 @@ struct RmsArgs {
     const float* bias_partial;   // (full precision: conv layers fp64)
     int bias_chunks[4];
     int bias_first[4];           // in floats
+    unsigned long long* changes; // counted up: theta has changed
 };
 
 __device__ inline void rms_update(const RmsArgs& a, float& th, float g, float& vv, float& mm)
@@ -734,6 +735,7 @@ __global__ __launch_bounds__(256) void rmsprop_kernel(float* theta_, float* grad
         const int idx = (block - flat_blocks_) * 256 + tid;
         const int ch = idx / kRmsBiasLanes, j = idx % kRmsBiasLanes;
         const bool live = ch < 32 + 64 + 64 + 512;
+        if (idx == 0) atomicAdd(a.changes, 1ull);   // (nothing waits for it)
         int layer = 3, c = 0;
         size_t e = 0;
         if (ch < 32) { layer = 0; c = ch; e = a.off.b1 + c; }
@@ -763,13 +765,14 @@ __global__ __launch_bounds__(256) void rmsprop_kernel(float* theta_, float* grad
     }
 }
 
-// Builds every operand copy of theta from the fp32 master (after dqn_set_params).
+// Builds every operand copy of theta from the fp32 master (after dqn_set_params), and counts the change.
 template <typename T>
 __global__ __launch_bounds__(256) void build_copies_kernel(const float* __restrict__ theta, T* __restrict__ sh,
-                                                           T* __restrict__ bsh, Offsets off)
+                                                           T* __restrict__ bsh, Offsets off, uint64_t* changes)
 {
     const size_t e = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x;
     if (e >= off.total) return;
+    if (e == 0) ++*changes;
     const T val = from_float<T>(theta[e]);
     shadow_store<T>(sh, off, e, theta[e]);
     if (bsh) {
@@ -782,12 +785,13 @@ __global__ __launch_bounds__(256) void build_copies_kernel(const float* __restri
     }
 }
 
-// theta^- <- theta: fp32 master (bitwise) and the forward operand copy.
+// theta^- <- theta: fp32 master (bitwise) and the forward operand copy; `changes` counts it.
 template <typename T>
 __global__ __launch_bounds__(256) void target_copy_kernel(const float* __restrict__ theta, float* __restrict__ theta_t,
-                                                          const T* __restrict__ sh, T* __restrict__ sh_t, size_t n, size_t n_copy)
+                                                          const T* __restrict__ sh, T* __restrict__ sh_t, size_t n, size_t n_copy, uint64_t* changes)
 {
     const size_t i = blockIdx.x * static_cast<size_t>(blockDim.x) + threadIdx.x;
+    if (i == 0) ++*changes;
     if (i < n) theta_t[i] = theta[i];
     if (i < n_copy) sh_t[i] = sh[i];
 }

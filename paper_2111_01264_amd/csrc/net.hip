@@ -131,9 +131,11 @@ struct dqn_ctx {
     // the quantised actor (dqn_quantize_actor): levels and scales of fc1.w [512][3136] and fc2.w [A][512] (device layout), and the act step's intermediates
     int8_t *q8_w1 = nullptr, *q8_w2 = nullptr, *q8_x = nullptr;
     float *q8_s1 = nullptr, *q8_s2 = nullptr, *q8_sx = nullptr, *q8_hidden = nullptr;
-    // theta (0) and theta^- (1) change: how often they have, and at which count the levels were made (0: never).  Those of theta are read and written under online_mu.
+    // theta (0) and theta^- (1) change: how often they have, and at which count the levels were made (0: never).  Twice: as calls were made, for the error that a caller gets, and as
+    // the device ran them (q8_state: both counts, then both marks), for calls in graphs, which run later, again or never.  A mark belongs to the calls that act.
     std::atomic<uint64_t> changes[2] = {{1}, {1}};
     uint64_t q8_at[2] = {0, 0};
+    uint64_t* q8_state = nullptr;
     // per-kernel timing (dqn_profile_*)
     int prof_id = 0;
     std::vector<hipEvent_t> prof_events;   // pairs
@@ -403,9 +405,10 @@ static int q8_act(dqn_ctx* c, const uint8_t* states, int W, int use_target, floa
     constexpr int kType = std::is_same<T, bf16_t>::value ? DQN_TYPE_BF16 : DQN_TYPE_FP32;
     rc = enqueue_quantize_rows(c->act_ws.act3, kType, 3136, W, 3136, c->q8_x, 3136, c->q8_sx, nullptr, 0, st);
     if (rc != DQN_OK) return rc;
+    const int which = use_target ? 1 : 0;
     rc = enqueue_q8_linear(c->q8_x, 3136, c->q8_sx, c->q8_w1, 3136, c->q8_s1, master[0] + o.bf1, true, W, 512, 3136, c->q8_hidden, DQN_TYPE_FP32, 512, st);
     if (rc != DQN_OK) return rc;
-    return enqueue_policy_q8_head(policy, c->q8_hidden, c->q8_w2, c->q8_s2, master[0] + o.bf2, q, W, st);
+    return enqueue_policy_q8_head(policy, c->q8_hidden, c->q8_w2, c->q8_s2, master[0] + o.bf2, c->q8_state + 2 + which, c->q8_state + which, q, W, st);
 }
 
 template <typename T>
@@ -590,6 +593,7 @@ static int train_impl(dqn_ctx* c, const uint8_t* s, const int32_t* a, const floa
         ra.lr = c->cfg.lr; ra.alpha = c->cfg.rms_alpha; ra.eps = c->cfg.rms_eps; ra.centered = c->cfg.centered;
         ra.bias_partial = c->bias_partial;
         for (int l = 0; l < 4; ++l) { ra.bias_chunks[l] = bias_chunks[l]; ra.bias_first[l] = bias_first[l]; }
+        ra.changes = reinterpret_cast<unsigned long long*>(c->q8_state);
         const int flat_blocks = static_cast<int>(((o.total - o.wf2) / 4 + 4 + 255) / 256);
         const uint32_t splits = static_cast<uint32_t>(wg_splits[0] | wg_splits[1] << 8 | wg_splits[2] << 16);   // at most 128, 64, 64
         launch_timed(rmsprop_kernel<T>, dim3(kRmsFc1Tiles + kRmsConvBlocks + flat_blocks + kRmsBiasBlocks), dim3(256), 0, st, pr.begin, pr.end, ra.theta, ra.grad, ra.v, ra.m,
@@ -597,6 +601,13 @@ static int train_impl(dqn_ctx* c, const uint8_t* s, const int32_t* a, const floa
         DQN_LAUNCH_CHECK();
     }
     return DQN_OK;
+}
+
+// The levels in the buffers are those of network `which` as it is now.
+__global__ void levels_made_kernel(uint64_t* state, int which)
+{
+    state[2 + which] = state[which];
+    state[3 - which] = 0;
 }
 
 // Public blob (OIHW, fc1 input index c*49 + h*7 + w)  <->  device layout (see gemm_mfma.h): the element of the public blob
@@ -719,6 +730,9 @@ int dqn_create(const dqn_config* cfg, void* act_stream, void* train_stream, dqn_
         DQN_HIP(hipMalloc((void**)&c->q8_s2, A * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->q8_sx, E * sizeof(float)));
         DQN_HIP(hipMalloc((void**)&c->q8_hidden, E * 512 * sizeof(float)));
+        const uint64_t state[4] = {1, 1, 0, 0};
+        DQN_HIP(hipMalloc((void**)&c->q8_state, sizeof(state)));
+        DQN_HIP(hipMemcpy(c->q8_state, state, sizeof(state), hipMemcpyHostToDevice));
         for (int i = 0; i < 2; ++i) {
             DQN_HIP(hipMalloc((void**)&c->mb_s[i], B * kStateBytes));
             DQN_HIP(hipMalloc((void**)&c->mb_s2[i], B * kStateBytes));
@@ -757,7 +771,7 @@ int dqn_destroy(dqn_ctx* c)
     (void)hipFree(c->dqv); (void)hipFree(c->lossv); (void)hipFree(c->loss_keep);
     (void)hipFree(c->bsh); (void)hipFree(c->bias_partial); (void)hipFree(c->wg_partial);
     (void)hipFree(c->q8_w1); (void)hipFree(c->q8_w2); (void)hipFree(c->q8_x); (void)hipFree(c->q8_s1); (void)hipFree(c->q8_s2);
-    (void)hipFree(c->q8_sx); (void)hipFree(c->q8_hidden);
+    (void)hipFree(c->q8_sx); (void)hipFree(c->q8_hidden); (void)hipFree(c->q8_state);
     for (int i = 0; i < 2; ++i) {
         (void)hipFree(c->mb_s[i]); (void)hipFree(c->mb_s2[i]); (void)hipFree(c->mb_a[i]); (void)hipFree(c->mb_r[i]); (void)hipFree(c->mb_d[i]);
         (void)hipFree(c->mb_desc[i]);
@@ -790,9 +804,9 @@ int dqn_set_params(dqn_ctx* c, int which, const float* host_src, size_t n)
         c->changes[online ? 0 : 1].fetch_add(1, std::memory_order_acq_rel);
         void *sh = online ? c->sh : c->sh_t, *bsh = online ? c->bsh : nullptr;
         if (c->cfg.precision == DQN_PRECISION_BF16)
-            hipLaunchKernelGGL(build_copies_kernel<bf16_t>, dim3(blocks), dim3(256), 0, c->train_stream, dst, static_cast<bf16_t*>(sh), static_cast<bf16_t*>(bsh), c->off);
+            hipLaunchKernelGGL(build_copies_kernel<bf16_t>, dim3(blocks), dim3(256), 0, c->train_stream, dst, static_cast<bf16_t*>(sh), static_cast<bf16_t*>(bsh), c->off, c->q8_state + (online ? 0 : 1));
         else
-            hipLaunchKernelGGL(build_copies_kernel<float>, dim3(blocks), dim3(256), 0, c->train_stream, dst, static_cast<float*>(sh), static_cast<float*>(bsh), c->off);
+            hipLaunchKernelGGL(build_copies_kernel<float>, dim3(blocks), dim3(256), 0, c->train_stream, dst, static_cast<float*>(sh), static_cast<float*>(bsh), c->off, c->q8_state + (online ? 0 : 1));
         DQN_LAUNCH_CHECK();
     }
     DQN_HIP(hipStreamSynchronize(c->train_stream));
@@ -909,6 +923,8 @@ int dqn_quantize_actor(dqn_ctx* c, int32_t use_target)
     if (rc != DQN_OK) return rc;
     rc = enqueue_quantize_rows(theta + c->off.wf2, DQN_TYPE_FP32, 512, c->A, 512, c->q8_w2, 512, c->q8_s2, nullptr, 0, c->act_stream);
     if (rc != DQN_OK) return rc;
+    hipLaunchKernelGGL(levels_made_kernel, dim3(1), dim3(1), 0, c->act_stream, c->q8_state, which);
+    DQN_LAUNCH_CHECK();
     c->q8_at[which] = c->changes[which].load(std::memory_order_acquire);
     if (!use_target) {
         DQN_HIP(hipEventRecord(c->ev_act, c->act_stream));
@@ -1097,9 +1113,9 @@ int dqn_sync_target(dqn_ctx* c, replay* rb, int32_t blocking)
     const size_t n = c->off.total, n_copy = copy_elements(c->off, c->esize);
     const dim3 grid(static_cast<unsigned>((n_copy + 255) / 256)), block(256);
     if (c->cfg.precision == DQN_PRECISION_BF16)
-        hipLaunchKernelGGL(target_copy_kernel<bf16_t>, grid, block, 0, c->train_stream, c->theta, c->theta_t, static_cast<const bf16_t*>(c->sh), static_cast<bf16_t*>(c->sh_t), n, n_copy);
+        hipLaunchKernelGGL(target_copy_kernel<bf16_t>, grid, block, 0, c->train_stream, c->theta, c->theta_t, static_cast<const bf16_t*>(c->sh), static_cast<bf16_t*>(c->sh_t), n, n_copy, c->q8_state + 1);
     else
-        hipLaunchKernelGGL(target_copy_kernel<float>, grid, block, 0, c->train_stream, c->theta, c->theta_t, static_cast<const float*>(c->sh), static_cast<float*>(c->sh_t), n, n_copy);
+        hipLaunchKernelGGL(target_copy_kernel<float>, grid, block, 0, c->train_stream, c->theta, c->theta_t, static_cast<const float*>(c->sh), static_cast<float*>(c->sh_t), n, n_copy, c->q8_state + 1);
     DQN_LAUNCH_CHECK();
     c->changes[1].fetch_add(1, std::memory_order_acq_rel);
     DQN_HIP(hipEventRecord(c->ev_sync, c->train_stream));

@@ -16,7 +16,8 @@ struct PolicyArgs {
 int enqueue_policy_sample(const PolicyArgs& a, int32_t type, int64_t rows, void* work, hipStream_t st);
 
 // The quantised actor's head: rows of 512 hidden values as q8_quantize_rows makes levels of them, their products with fc2's levels [n][512] as q8_linear makes Q rows, into
-// q [rows][n], and the draw from them (a.scores is not read; n <= 32).
-int enqueue_policy_q8_head(const PolicyArgs& a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q, int64_t rows, hipStream_t st);
+// q [rows][n], and the draw from them (a.scores is not read; n <= 32).  Where *made != *now (the levels are not those of the present parameters) q and logp are NaN and the index is -1.
+int enqueue_policy_q8_head(const PolicyArgs& a, const float* hidden, const int8_t* w, const float* scales, const float* bias, const uint64_t* made, const uint64_t* now,
+                           float* q, int64_t rows, hipStream_t st);
 
 }  // namespace dqn

@@ -170,13 +170,15 @@ __global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t
 
 // A workgroup per row: two hidden values per thread become levels in LDS, eight threads sum the products of one action, the first wavefront draws.  Nothing but the chain of launches bounds
 // a call this small, and this is one instead of three (act step of 8 states, bf16: 25 us with three, 17 to 20 with one).
-__global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q)
+__global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const float* hidden, const int8_t* w, const float* scales, const float* bias, const uint64_t* made, const uint64_t* now,
+                                                              float* q)
 {
     __shared__ uint32_t part[4];
     __shared__ alignas(16) int8_t levels[512];
     __shared__ float scores[32];
     const int64_t row = blockIdx.x;
     const int t = threadIdx.x;
+    const bool current = *made == *now;   // else the row's scale is NaN, and with it all that follows
     typedef float f32x2 __attribute__((ext_vector_type(2)));
     const f32x2 h = reinterpret_cast<const f32x2*>(hidden + row * 512)[t];
     uint32_t top = max(magnitude(h[0]), magnitude(h[1]));
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const
     __syncthreads();
     top = max(max(part[0], part[1]), max(part[2], part[3]));
     const bool finite = top < 0x7F800000u;
-    const float m = finite ? __uint_as_float(top) : 0.f, s = finite ? row_scale(m) : not_a_number();
+    const float m = finite ? __uint_as_float(top) : 0.f, s = finite && current ? row_scale(m) : not_a_number();
     const Levels l = make_levels(m);
     levels[2 * t] = static_cast<int8_t>(finite ? level_of(l, h[0]) : 0);
     levels[2 * t + 1] = static_cast<int8_t>(finite ? level_of(l, h[1]) : 0);
@@ -1094,9 +1096,10 @@ template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows
     return DQN_OK;
 }
 
-int enqueue_policy_q8_head(const PolicyArgs& a, const float* hidden, const int8_t* w, const float* scales, const float* bias, float* q, int64_t rows, hipStream_t st)
+int enqueue_policy_q8_head(const PolicyArgs& a, const float* hidden, const int8_t* w, const float* scales, const float* bias, const uint64_t* made, const uint64_t* now,
+                           float* q, int64_t rows, hipStream_t st)
 {
-    hipLaunchKernelGGL(policy_q8_head_kernel, dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, hidden, w, scales, bias, q);
+    hipLaunchKernelGGL(policy_q8_head_kernel, dim3(static_cast<unsigned>(rows)), dim3(256), 0, st, a, hidden, w, scales, bias, made, now, q);
     DQN_LAUNCH_CHECK();
     return DQN_OK;
 }
