@@ -33,7 +33,7 @@ int fail(int code, const char* fmt, ...);
 inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 inline bool aligned16(const void* p) { return aligned_to(p, 16); }
 
-// Allows a kernel `bytes` of dynamic LDS, beyond the default limit, on the current device; remembered per kernel and device.
+// Allows a kernel `bytes` of dynamic LDS, beyond the default limit, on the current device; the largest amount is remembered per kernel and device.
 hipError_t raise_dynamic_lds(const void* kernel, int bytes);
 
 // Argument checks of the calls that belong to no handle: an element type; a stream of the current device (the launch goes there).

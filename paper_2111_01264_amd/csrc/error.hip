@@ -22,19 +22,19 @@ int fail(int code, const char* fmt, ...)
 
 hipError_t raise_dynamic_lds(const void* kernel, int bytes)
 {
-    constexpr int kKernels = 64;
+    constexpr int kKernels = 64, kDevices = 64;   // (beyond these nothing is remembered, and the runtime is asked every time)
     static std::mutex mu;
-    static struct { const void* kernel; uint64_t devices; } done[kKernels];   // (the library has fewer such kernels)
+    static struct { const void* kernel; int bytes[kDevices]; } allowed[kKernels];
     int device = 0;
     const hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return e;
-    const uint64_t bit = 1ull << (device & 63);
     std::lock_guard<std::mutex> lock(mu);
     int i = 0;
-    while (i < kKernels && done[i].kernel && done[i].kernel != kernel) ++i;
-    if (i < kKernels && done[i].kernel == kernel && (done[i].devices & bit)) return hipSuccess;
+    while (i < kKernels && allowed[i].kernel && allowed[i].kernel != kernel) ++i;
+    const bool known = i < kKernels && device >= 0 && device < kDevices;
+    if (known && allowed[i].kernel == kernel && allowed[i].bytes[device] >= bytes) return hipSuccess;
     const hipError_t r = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (r == hipSuccess && i < kKernels) { done[i].kernel = kernel; done[i].devices |= bit; }
+    if (r == hipSuccess && known) { allowed[i].kernel = kernel; allowed[i].bytes[device] = bytes; }
     return r;
 }
 
