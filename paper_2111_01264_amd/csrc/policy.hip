@@ -827,7 +827,7 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
     }
     if (by_digits) {
         last = 0;
-        uint64_t floor = st.m == INFINITY ? static_cast<uint64_t>(score_key(INFINITY)) << 32 : 0;   // beside +infinity nothing has mass
+        const uint64_t floor = st.m == INFINITY ? entry_of(INFINITY, 0x7FFFFFFF) : 0;   // beside +infinity nothing has mass: its last entry, behind every index
 #pragma unroll 1
         for (int filter = 0; filter < 2; ++filter) {
             if (filter == 0 ? !s.k : !(s.p < 1.0)) continue;
