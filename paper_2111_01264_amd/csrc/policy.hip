@@ -876,13 +876,14 @@ struct SplitRow {
     uint32_t count[2];   // entries in the lists: the last kept one is among the second where both filters are on, top-k's border in the first
 };
 
-// A launch costs about 4 us, so the rows have to be long (and few: they share the compute units).  One workgroup per row against this, bf16: 32768 scores, one row,
-// temperature alone 23 / 25 us, top-p 45 / 43, top-k 50 18 / 26; 65536: 34 / 24, 70 / 45, 22 / 26; 131072: 54 / 25, 117 / 49, 29 / 26; 64 rows of it: 57 / 41, 122 / 81, 30 / 31.
+// A launch costs about 4 us, so the rows have to be long, and few: they share the compute units, and from 65 on each has three workgroups at most.  One workgroup per row against this,
+// bf16, in us: one row of 32768, temperature alone 28 / 27, top-p 45 / 44, top-k 50 20 / 26; of 49152: 32 / 25, 52 / 43, 23 / 29; of 131072: 51 / 27, 89 / 48, 31 / 26; 64 rows of
+// 131072: 54 / 44, 97 / 87, 33 / 33; 72 rows: 54 / 54, 94 / 100, 33 / 39; 128 rows: 54 / 62, 96 / 121, 33 / 38.
 struct SplitPlan { int parts, len, groups; };   // len: scores of a part, groups per part
 static SplitPlan split_plan(int64_t rows, int64_t n)
 {
     SplitPlan p{1, static_cast<int>(n), 0};
-    if (rows < 1 || rows > 128 || n < 12 * kPartMin) return p;
+    if (rows < 1 || rows > 64 || n < 12 * kPartMin) return p;
     int64_t parts = n / kPartMin;
     if (parts > 256 / rows) parts = 256 / rows;
     if (parts > kParts) parts = kParts;

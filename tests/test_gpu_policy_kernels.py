@@ -10,7 +10,7 @@ import paper_2111_01264_amd as P
 from tests.gpu_kernels import kernels_of
 from tests.test_gpu_policy_sample import INF, NAN, TYPES, Call, gen
 
-N = 60000   # shared out, at up to 128 rows
+N = 60000   # shared out, at up to 64 rows
 
 
 def shared_out(call):
