@@ -1072,7 +1072,6 @@ __global__ __launch_bounds__(kPartThreads) void policy_split_kernel(PolicyArgs a
 
 template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows, void* work, hipStream_t st)
 {
-    constexpr int E = 16 / sizeof(T);
     const SplitPlan plan = split_plan(rows, a.n);
     const dim3 grid(static_cast<unsigned>(rows));
     if (plan.parts > 1) {
@@ -1086,8 +1085,12 @@ template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows
         }
         return DQN_OK;
     }
+    // (a workgroup for each row of 64 scores: 512 rows temperature alone 8.4 us, this way 3.7; top-p 14 and 7.7)
     if (a.n <= 64) hipLaunchKernelGGL(policy_short_kernel<T>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, rows);
-    else if (a.n <= 256 * E * 8) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
+    // Four workgroups of 256 threads fit a compute unit, one of 1024: with more rows than compute units the small ones win up to longer rows.  256 / 1024 threads, in us, temperature
+    // alone, top-p, top-k 50; 256 rows fp32: 8192 scores 15 / 23, 26 / 35, 19 / 19; 16384: 20 / 27, 37 / 41, 22 / 21; 24576: 25 / 29, 49 / 47, 24 / 22; bf16 alike (16384: 19 / 28,
+    // 38 / 41, 20 / 20).  512 rows fp32: 16384: 25 / 48, 45 / 76, 24 / 37; 49152: 58 / 73, 110 / 131, 44 / 55; bf16: 49152: 51 / 69, 110 / 112, 37 / 49; 65536: 66 / 76, 142 / 127, 43 / 53.
+    else if (a.n <= (rows > 256 ? 49152 : 16384)) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
     else {
         constexpr int smem = kWithTable<T, 1024> ? kTablePlaces * static_cast<int>(sizeof(uint64_t)) : 0;
         if (smem) DQN_HIP(raise_dynamic_lds(reinterpret_cast<const void*>(policy_row_kernel<T, 1024>), smem));
