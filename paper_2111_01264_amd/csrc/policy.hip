@@ -226,6 +226,10 @@ __global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const
 // 300 KB.  A wavefront has a contiguous stretch, so that the draw, a search in index order, goes from a quarter of such a stretch to one score.  What
 // bounds it are the exponentials: 25 instructions at fp64's rate for each.
 constexpr int kListK = 192, kPolicyGroups = 512;
+// The largest k for which the groups' way is taken.  The nearer k comes to the number of groups, the lower its bound and the longer its list; what it saves is a pass over the row with
+// exponentials.  Groups / range, in us, 64 rows: 1000 scores k = 48 13 / 13, 96 19 / 13; 4096: 64 16 / 16, 96 21 / 17; 8192: 80 21 / 21, 128 26 / 21; 16384: 128 28 / 31 (bf16; fp32 27 / 35),
+// 160 33 / 31; 32768: 192 38 / 43; 256 rows of 131072: 192 60 / 87 (fp32 83 / 119).
+__device__ inline int list_most(int n) { return min(kListK, 48 + n / 192); }
 
 // (sized by the threads: four workgroups of 256 threads fit a compute unit)
 template <int THREADS> struct RowShared {
@@ -406,7 +410,7 @@ struct RowState {
     // (rounding is monotone)
     template <int BINS> __device__ __forceinline__ int bin(float x) const { return min(static_cast<int>((m - x) * per), BINS - 1); }
 };
-template <int BINS> __device__ inline RowState row_state(const RowSettings& s, float hi, float low, bool nan)
+template <int BINS> __device__ inline RowState row_state(const RowSettings& s, float hi, float low, bool nan, int list_k)
 {
     RowState st;
     st.m = uniform(hi);
@@ -415,7 +419,7 @@ template <int BINS> __device__ inline RowState row_state(const RowSettings& s, f
     st.lo = uniform(fmaxf(low, static_cast<float>(fmax(static_cast<double>(hi) - 28.5 * s.t, -0x1.fffffep127)) - 2e-7f * fabsf(hi)));
     st.per = uniform(fminf(static_cast<float>(BINS) / (st.m - st.lo), 0x1.fffffep127f));
     const bool flat = !(st.lo < st.m) || st.m - st.lo == INFINITY;   // no range to divide
-    st.way = s.bad || nan || st.m == -INFINITY ? Way::kRefused : s.greedy ? Way::kGreedy : s.k && s.k <= kListK ? Way::kShortList
+    st.way = s.bad || nan || st.m == -INFINITY ? Way::kRefused : s.greedy ? Way::kGreedy : s.k && s.k <= list_k ? Way::kShortList
            : !s.k && !(s.p < 1.0) ? Way::kPlain : flat ? Way::kDigits : Way::kRange;
     return st;
 }
@@ -479,7 +483,8 @@ template <int THREADS, typename ROW> __device__ __forceinline__ bool extremes(Ro
     return nan;
 }
 
-// How many groups: enough that the entries above the k-th largest maximum are few more than k, few enough to rank.
+// How many groups: enough that the entries above the k-th largest maximum are few more than k, few enough to rank (this / always 256, in us: 512 rows of 1000 fp32 scores, k = 20
+// 11 / 15, 40 14 / 16, 64 16 / 18; 256 rows of 16384: 20 17 / 19, 64 21 / 22).
 __device__ __host__ inline int groups_for(int k) { return k <= 24 ? 64 : k <= 64 ? 128 : 256; }
 
 // The k-th largest of sh.group[0 .. n).
@@ -773,11 +778,11 @@ template <typename T, int THREADS> __device__ __forceinline__ void whole_row(Row
     const ROW row(a, r, 0, a.n);
     const RowSettings s = row_settings(a, r);
     float hi, low;
-    const int groups = groups_for(s.k);
+    const int groups = groups_for(s.k), list_k = list_most(a.n);
     bool others = false;
-    uint32_t* counts = !s.greedy && (s.k > kListK || (!s.k && s.p < 1.0)) ? reinterpret_cast<uint32_t*>(table) : nullptr;   // (for the histogram)
+    uint32_t* counts = !s.greedy && (s.k > list_k || (!s.k && s.p < 1.0)) ? reinterpret_cast<uint32_t*>(table) : nullptr;   // (for the histogram)
     const bool nan = extremes<THREADS>(sh, row, &hi, &low, sh.group, groups, counts, &others);
-    const RowState st = row_state<RowShared<THREADS>::BINS>(s, hi, low, nan);
+    const RowState st = row_state<RowShared<THREADS>::BINS>(s, hi, low, nan, list_k);
     if (st.way == Way::kRefused) {
         if (threadIdx.x == 0) answer(a, r, -1, not_a_number());
         return;
@@ -864,6 +869,8 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(PolicyArgs a)
 //   3  draw (short list, no filter) | entries of the part of the range that the last kept one lies in, kept mass above it        4  draw
 // A row that the list or the range cannot hold is done by one workgroup in the last launch.
 constexpr int kParts = 64, kPartThreads = 1024, kPartMin = 4096;
+// (as list_most: one row of 65536, k = 96 31 / 42 us in bf16, 128 43 / 42, 160 56 / 42, where equal scores overflow the list; fp32 128 32 / 42, 160 39 / 42, 192 41 / 42)
+constexpr int kPartListK = 128;
 typedef RowShared<kPartThreads> PartShared;
 
 struct SplitRow {
@@ -919,7 +926,7 @@ __global__ __launch_bounds__(kPartThreads) void policy_split_kernel(PolicyArgs a
     if (row.lane < plan.parts) { hi = rec.hi[row.lane]; low = rec.low[row.lane]; nan = rec.nan[row.lane] != 0; }
     for (int d = 32; d; d >>= 1) { hi = max(hi, static_cast<uint32_t>(__shfl_xor(static_cast<int>(hi), d))); low = min(low, static_cast<uint32_t>(__shfl_xor(static_cast<int>(low), d))); }
     nan = __any(nan);
-    const RowState st = row_state<BINS>(s, key_score(hi), key_score(low), nan);
+    const RowState st = row_state<BINS>(s, key_score(hi), key_score(low), nan, kPartListK);
     const bool both = s.k && s.p < 1.0;
     // the part that u's share of the kept mass falls into, given all parts' kept mass in sh.mass: its workgroup draws
     auto draw_in_part = [&](uint64_t last) {
