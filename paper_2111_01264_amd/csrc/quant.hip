@@ -457,12 +457,13 @@ template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
 {
     const auto blocks = [&](int bn, int bm) { return dim3(static_cast<unsigned>((a.N + bn - 1) / bn), static_cast<unsigned>((a.M + bm - 1) / bm)); };
     const auto tiles = [&](int64_t t) { return (a.M + t - 1) / t * ((a.N + t - 1) / t); };
-    // Up to 16 rows of x, and where tiles of 64 would leave half of the chip idle: streamed, in tiles of 16 while there are few of 32 (16 / 32: 128x512x3136 4.8 / 7.0 us, 200x300x16384
-    // 17 / 31; 384x512x3136 9.0 / 6.9, 512x512x3136 9.9 / 7.1).  A short k has four wavefronts, a longer one eight (1x65536x1024 13 us with four, 18
-    // with eight; 1x16384x4096 17 and 13).
-    if (a.M <= 16 || tiles(64) < 128) {
+    // Streamed: up to 16 rows of x, and while there are no more pieces of 32 than compute units (32 / tiles of 64, in us: 512x512 1024 6.0 / 6.5, 3136 7.8 / 10.8, 8192 18.9 / 31.7; 32x8000
+    // 3136 7.7 / 10.7; 512x576 1024 9.5 / 6.3, 3136 13.0 / 10.8, 8192 34.7 / 31.8).  In pieces of 16 while there are few of 32 (16 / 32: 128x512x3136 4.2 / 6.8, 128x1024x3136 6.6 / 7.5,
+    // 200x300x16384 17.5 / 31.6, 352x512 k 512 4.3 / 5.0 and 3136 8.4 / 7.6, 384x512x3136 8.5 / 7.5).  A short k has four wavefronts, a longer one eight (4 / 8: 1x65536 k 1024
+    // 13.3 / 18.6, 3136 30.4 / 33.7, 4096 48.8 / 46.0; 1x16384 k 3600 11.2 / 11.5, 4096 15.4 / 13.8, 8192 24.9 / 23.7; 8x512x3136 alike).
+    if (a.M <= 16 || tiles(32) <= 256) {
         const bool by_16 = a.M <= 16 || tiles(32) < 192;
-        if (by_16 && a.K < 2048) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
+        if (by_16 && a.K < 4096) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 4>), blocks(16, 16), dim3(256), 0, st, a);
         else if (by_16) hipLaunchKernelGGL((q8_stream_kernel<T, 16, 4, 8>), blocks(16, 16), dim3(512), 0, st, a);
         else hipLaunchKernelGGL((q8_stream_kernel<T, 32, 8, 8>), blocks(32, 32), dim3(512), 0, st, a);
         DQN_LAUNCH_CHECK();
@@ -470,10 +471,11 @@ template <typename T> static int launch_linear(const Q8Args& a, hipStream_t st)
     }
     // 16-byte loads straight into LDS need rows on 16-byte borders; a lane's place within a tile is a 32-bit offset
     const bool aligned = aligned16(a.x) && aligned16(a.w) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.ldx < (1 << 23) && a.ldw < (1 << 23);
-    // The largest tile of which there are enough: a smaller one reads its operands more often, a larger one leaves compute units idle (64 / 128: 1111x2051x2003 18 / 19 us, 1024^3 6.5 / 9.8, 2048^3
-    // 19.7 / 16.6, 256x16384x4096 36 / 28; 128 / 256: 8192^3 packed, where there is no 256, 1105 us, 600 with).
+    // The largest tile of which there are enough: a smaller one reads its operands more often, a larger one leaves compute units idle (64 / 128, in us: 1024^3 8.1 / 11.6, 1111x2051x2003 20 / 24,
+    // 1536x2048x2048 16 / 19, 1792x1792x2048 19.6 / 18.6, 2048^3 20.4 / 18.0, 256x16384x4096 35 / 33).  One of 256 starts and ends slower, which a long k makes up for (128 / 256 on the same
+    // aligned operands: 8192x8192 k 1024 111 / 149, 4096 295 / 301, 8192 542 / 500; 4096x4096 k 4096 80 / 85, 8192 141 / 137, 16384 266 / 240; 3328x3328 k 4096 66 / 64, 8192 113 / 105).
     if (tiles(128) < 200) return aligned ? launch_tile<T, 64, 256, true>(a, st) : launch_tile<T, 64, 256, false>(a, st);
-    if (tiles(256) < 192) return aligned ? launch_tile<T, 128, 256, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
+    if (tiles(256) < 160 || a.K < 6144) return aligned ? launch_tile<T, 128, 256, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
     return aligned ? launch_tile<T, 256, 512, true>(a, st) : launch_tile<T, 128, 256, false>(a, st);
 }
 

@@ -12,10 +12,10 @@ from tests.test_gpu_q8_linear import TYPES, check, gen, levels, run, wanted
 
 # kernel: M, N, K that reach it on rows of their own length, padded to 16 bytes where `aligned`
 SIZES = {
-    "q8_stream_kernel 16 4 4": (9, 1000, 700), "q8_stream_kernel 16 4 8": (5, 500, 2100), "q8_stream_kernel 32 8 8": (500, 480, 300),
+    "q8_stream_kernel 16 4 4": (9, 1000, 700), "q8_stream_kernel 16 4 8": (5, 500, 4100), "q8_stream_kernel 32 8 8": (500, 512, 300),
     "q8_tile_kernel 64 256 1": (1000, 1003, 200), "q8_tile_kernel 64 256 0": (1000, 1003, 200),
     "q8_tile_kernel 128 256 1": (2003, 2000, 100), "q8_tile_kernel 128 256 0": (2003, 2000, 100),
-    "q8_tile_kernel 256 512 1": (3600, 3601, 140),
+    "q8_tile_kernel 256 512 1": (3600, 3601, 6150),
 }
 
 
@@ -71,7 +71,12 @@ def pitches(kernel, K, extra=0):
 @pytest.mark.parametrize("kernel", list(SIZES))
 def test_lengths_of_k(kernel, kind):
     M, N, K0 = SIZES[kernel]
-    Ks = (K0, K0 + 1, K0 + 64) if "stream" in kernel else (K0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 191, 193, 256, 320, 384, 449, 513, 640)
+    if "stream" in kernel:
+        Ks = (K0, K0 + 1, K0 + 64)
+    elif " 256 512 " in kernel:   # every kind of rest behind whole pairs of steps
+        Ks = (K0, 6144, 6145, 6159, 6160, 6161, 6207, 6208, 6209, 6271, 6272, 6273)
+    else:
+        Ks = (K0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 191, 193, 256, 320, 384, 449, 513, 640)
     for K in Ks:
         ld = pitches(kernel, K)
         p = Product(M, N, K, kind, ld, ld).reach(kernel)
