@@ -117,7 +117,12 @@ template <typename T> static void launch_quantize(const QuantArgs& a, hipStream_
         const int rpb = tpr < 256 ? 256 / tpr : 1;
         hipLaunchKernelGGL(kern, dim3(static_cast<unsigned>((a.rows + rpb - 1) / rpb)), dim3(tpr < 256 ? 256 : tpr), 0, st, a);
     };
+    // The smallest workgroup that holds a row in few vectors, but all of a compute unit's threads for a row where rows are few.  Levels alone, in us, 64 / 256 threads: 8192 rows of 1024 bf16
+    // 9.8 / 13.0; 256 with four / eight vectors: 8192 rows of 8192 43.7 / 44.0; 256 / 1024: 32 rows of 2048 3.4 / 3.7, of 3136 4.3 / 3.8, of 8192 6.0 / 4.7, of 16384 12.7 / 6.9; 512 rows of
+    // 3136 5.4 / 5.5, of 8192 8.4 / 7.1, of 16384 14.6 / 11.2; 1024 of 8192 10.5 / 11.4, of 16384 20 / 18; 2048 of 8192 17.6 / 19.5; 8192 of 8192 44 / 63.  Read once / twice: 1024 rows of
+    // 65536 54 / 58, fp32 of 32768 35 / 44.
     if (vecs <= 64 * 2) go(quantize_rows_kernel<T, 64, 2>, 64);
+    else if (a.rows <= 512 && vecs > 384 && vecs <= 1024 * 8) go(quantize_rows_kernel<T, 1024, 8>, 1024);
     else if (vecs <= 256 * 4) go(quantize_rows_kernel<T, 256, 4>, 256);
     else if (vecs <= 256 * 8) go(quantize_rows_kernel<T, 256, 8>, 256);
     else if (vecs <= 1024 * 8) go(quantize_rows_kernel<T, 1024, 8>, 1024);
