@@ -298,7 +298,9 @@ int q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, in
  * Scores of -infinity are never drawn; scores of +infinity share the whole mass.  A row without a score above -infinity (n = 0 among them),
  * one that holds a NaN, a temperature that is negative or not finite, or a NaN in top_p, min_p or u gives index -1 and logp NaN.
  * Weights are held as whole multiples of 2^-40 of the largest, from fp64 exponentials: sums do not depend on their order, and the result is the
- * same on every run.
+ * same on every run.  What that costs: a mass of n entries, at least 1 in units of the largest weight, is off by up to n 2^-41 (2^-19 for the longest row), so
+ * logp is off by as much beside its rounding to fp32, as are the borders that top_p and u are compared with; and an entry that lies more than 28.4 T
+ * below the largest has no weight and is never drawn.
  * work: device memory of at least policy_sample_workspace(rows, n) bytes (NULL where that is 0), 16-byte aligned; it needs no
  * clearing, and two calls that may overlap in time (on two streams, or in two graphs) need one each.  Errors: DQN_EINVAL (type, rows outside
  * 0..4194303, n outside 0..4194304, ld < n, null / misaligned pointer, work too small). */
