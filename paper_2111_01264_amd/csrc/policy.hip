@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256) void policy_short_kernel(PolicyArgs a, int64_t
 }
 
 // A workgroup per row: two hidden values per thread become levels in LDS, eight threads sum the products of one action, the first wavefront draws.  Nothing but the chain of launches bounds
-// a call this small, and this is one instead of three (act step of 8 states, bf16: 25 us with three, 17 to 20 with one).
+// a call this small, and this is one instead of three (act step of 8 states, bf16: 25 us with three, 17 to 20 with one, from run to run: the host's share of its launches).
 __global__ __launch_bounds__(256) void policy_q8_head_kernel(PolicyArgs a, const float* hidden, const int8_t* w, const float* scales, const float* bias, const uint64_t* made, const uint64_t* now,
                                                               float* q)
 {
@@ -425,7 +425,7 @@ template <int BINS> __device__ inline RowState row_state(const RowSettings& s, f
 }
 
 // bf16 scores have few values: all those from 2^-24 to 2^8 and their negatives have a place in a table in LDS, so that a long row needs an exponential per value instead of one per
-// score.  Others (rare) are treated one by one.  256 rows of 131072, top-p: 131 -> 103 us; one compute unit's LDS holds one workgroup then, which a row this long fills anyway.
+// score.  Others (rare) are treated one by one.  256 rows of 131072, top-p: 131 -> 103 us, of which the counting takes 12 (first pass 26 us, fp16's without it 14; profiles/policy_row_passes.txt); one compute unit's LDS holds one workgroup then, which a row this long fills anyway.
 constexpr int kTablePlaces = 8192;
 __device__ __forceinline__ uint32_t table_place(bf16_t x)   // kTablePlaces or more: none
 {

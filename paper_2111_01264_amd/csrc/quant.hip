@@ -276,8 +276,9 @@ __global__ __launch_bounds__(WAVES * 64) void q8_stream_kernel(Q8Args a)
 // free.  A wavefront reads the operands of the next half step while it multiplies those of this one; there is one barrier per step, in the middle: behind it the
 // stage that everybody has read is free, and the next one is complete.  Rows that do not start on 16-byte borders (not ALIGNED) come through registers, a step ahead.
 //
-// 8192^3: 573 to 605 us, 1.9 PTOP/s; what bounds it is power: the matrix instructions are busy for 44 % of the cycles at a clock that has fallen to 1.9 GHz, levels that are all zero
-// take 448 us, the matrix instructions alone 435.  One wavefront per SIMD with parts of 128 x 128 takes as long as two of 128 x 64.  1111x2051x2003: 18 us, packed 27.6.
+// 8192^3: 550 to 615 us, 1.8 to 2.0 PTOP/s; what bounds it is power: the matrix instructions need 524 k cycles of each SIMD (218 us at 2.4 GHz), 54 % of the 967 k that a launch takes at a clock
+// of 1.65 GHz; levels that are all zero take 420 us (profiles/actor_operators_counters.txt).  One wavefront per SIMD with parts of 128 x 128 takes as long as two of 128 x 64.
+// 1111x2051x2003: 20 us, packed 28.
 //
 // A row's four 16-byte chunks are stored at the places c ^ swizzle(row), so that the 32 rows that one read takes the same chunk of do
 // not meet in the same banks.
