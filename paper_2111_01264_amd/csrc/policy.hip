@@ -1096,8 +1096,9 @@ template <typename T> static int launch_policy(const PolicyArgs& a, int64_t rows
     if (a.n <= 64) hipLaunchKernelGGL(policy_short_kernel<T>, dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(256), 0, st, a, rows);
     // Four workgroups of 256 threads fit a compute unit, one of 1024: with more rows than compute units the small ones win up to longer rows.  256 / 1024 threads, in us, temperature
     // alone, top-p, top-k 50; 256 rows fp32: 8192 scores 15 / 23, 26 / 35, 19 / 19; 16384: 20 / 27, 37 / 41, 22 / 21; 24576: 25 / 29, 49 / 47, 24 / 22; bf16 alike (16384: 19 / 28,
-    // 38 / 41, 20 / 20).  512 rows fp32: 16384: 25 / 48, 45 / 76, 24 / 37; 49152: 58 / 73, 110 / 131, 44 / 55; bf16: 49152: 51 / 69, 110 / 112, 37 / 49; 65536: 66 / 76, 142 / 127, 43 / 53.
-    else if (a.n <= (rows > 256 ? 49152 : 16384)) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
+    // 38 / 41, 20 / 20).  512 rows fp32: 16384: 25 / 48, 45 / 76, 24 / 37; 32768: 43 / 62, 79 / 103, 36 / 46; bf16: 32768: 37 / 58, 77 / 92, 29 / 41.  Beyond, a border among many scores may
+    // overflow the small workgroup's list (49152 Laplace-distributed scores, top-p: 280 / 117).
+    else if (a.n <= (rows > 256 ? 32768 : 16384)) hipLaunchKernelGGL((policy_row_kernel<T, 256>), grid, dim3(256), 0, st, a);
     else {
         constexpr int smem = kWithTable<T, 1024> ? kTablePlaces * static_cast<int>(sizeof(uint64_t)) : 0;
         if (smem) DQN_HIP(raise_dynamic_lds(reinterpret_cast<const void*>(policy_row_kernel<T, 1024>), smem));
