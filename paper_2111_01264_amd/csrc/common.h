@@ -36,9 +36,9 @@ inline bool aligned16(const void* p) { return aligned_to(p, 16); }
 // Allows a kernel `bytes` of dynamic LDS, beyond the default limit, on the current device; the largest amount is remembered per kernel and device.
 hipError_t raise_dynamic_lds(const void* kernel, int bytes);
 
-// Argument checks of the calls that belong to no handle: an element type; a stream of the current device (the launch goes there).
+// Argument checks of the calls that belong to no handle: an element type; a stream of the current device (the launch goes there: *out).
 int check_type(const char* who, int32_t type);
-int check_stream_device(const char* who, void* stream);
+int check_stream(const char* who, void* stream, hipStream_t* out);
 
 // Replay internals needed by dqn_sync_target.
 int replay_flush_ordered(replay* rb);

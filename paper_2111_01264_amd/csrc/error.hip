@@ -44,13 +44,15 @@ int check_type(const char* who, int32_t type)
     return DQN_OK;
 }
 
-int check_stream_device(const char* who, void* stream)
+int check_stream(const char* who, void* stream, hipStream_t* out)
 {
-    if (!stream) return DQN_OK;   // the null stream is the current device's
+    *out = static_cast<hipStream_t>(stream);
+    if (*out == hipStreamLegacy) *out = nullptr;   // its other name, which not every runtime's calls know: hipStreamGetDevice follows it as a pointer
+    if (!*out) return DQN_OK;   // the null stream is the current device's
     int current = -1;
     hipDevice_t owner = -1;
     DQN_HIP(hipGetDevice(&current));
-    DQN_HIP(hipStreamGetDevice(static_cast<hipStream_t>(stream), &owner));
+    DQN_HIP(hipStreamGetDevice(*out, &owner));
     if (owner != current) return fail(DQN_EINVAL, "%s: the stream belongs to device %d, the current device is %d", who, owner, current);
     return DQN_OK;
 }

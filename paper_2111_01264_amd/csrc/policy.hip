@@ -1146,9 +1146,10 @@ int policy_sample(const void* scores, int32_t type, int64_t ld, int64_t rows, in
         return fail(DQN_EINVAL, "%s: a pointer is not aligned to its elements", who);
     if (ld < n) return fail(DQN_EINVAL, "%s: ld = %lld is shorter than a row of %lld", who, (long long)ld, (long long)n);
     if (const size_t need = policy_sample_workspace(rows, n); need && (!work || work_bytes < need)) return fail(DQN_EINVAL, "%s: work holds %zu bytes, needed %zu", who, work ? work_bytes : 0, need);
-    if (int rc = check_stream_device(who, stream)) return rc;
+    hipStream_t st;
+    if (int rc = check_stream(who, stream, &st)) return rc;
     const PolicyArgs a{scores, ld, static_cast<int32_t>(n), temperature, top_k, top_p, min_p, u, 0, 0, index, logp};
-    return enqueue_policy_sample(a, type, rows, work, static_cast<hipStream_t>(stream));
+    return enqueue_policy_sample(a, type, rows, work, st);
 }
 
 }  // extern "C"

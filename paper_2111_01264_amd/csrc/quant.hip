@@ -509,8 +509,9 @@ int q8_quantize_rows(const void* x, int32_t type, int64_t ldx, int64_t rows, int
     const uintptr_t e = type == DQN_TYPE_FP32 ? 4 : 2;
     if (!aligned_to(x, e) || !aligned_to(values, e) || !aligned_to(scale, 4)) return fail(DQN_EINVAL, "%s: a pointer is not aligned to its elements", who);
     if (ldx < cols || (q && ldq < cols) || (values && ldv < cols)) return fail(DQN_EINVAL, "%s: a row pitch is shorter than a row", who);
-    if (int rc = check_stream_device(who, stream)) return rc;
-    return enqueue_quantize_rows(x, type, ldx, rows, cols, q, ldq, scale, values, ldv, static_cast<hipStream_t>(stream));
+    hipStream_t st;
+    if (int rc = check_stream(who, stream, &st)) return rc;
+    return enqueue_quantize_rows(x, type, ldx, rows, cols, q, ldq, scale, values, ldv, st);
 }
 
 int q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, int64_t ldw, const float* sw, const float* bias, int32_t relu, int64_t M, int64_t N,
@@ -525,8 +526,9 @@ int q8_linear(const int8_t* x, int64_t ldx, const float* sx, const int8_t* w, in
     if (!aligned_to(y, type == DQN_TYPE_FP32 ? 4 : 2) || !aligned_to(sx, 4) || !aligned_to(sw, 4) || !aligned_to(bias, 4))
         return fail(DQN_EINVAL, "%s: a pointer is not aligned to its elements", who);
     if (ldx < K || ldw < K || ldy < N) return fail(DQN_EINVAL, "%s: a row pitch is shorter than a row", who);
-    if (int rc = check_stream_device(who, stream)) return rc;
-    return enqueue_q8_linear(x, ldx, sx, w, ldw, sw, bias, relu != 0, M, N, K, y, type, ldy, static_cast<hipStream_t>(stream));
+    hipStream_t st;
+    if (int rc = check_stream(who, stream, &st)) return rc;
+    return enqueue_q8_linear(x, ldx, sx, w, ldw, sw, bias, relu != 0, M, N, K, y, type, ldy, st);
 }
 
 }  // extern "C"
