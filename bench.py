@@ -90,14 +90,14 @@ _WG_SRC = _sources("wgrad_all.h")
 _TOWER_SRC = _sources("conv_tower.h", "conv_tower_many.h")
 _TOWER_BWD_SRC = _sources("conv_tower_bwd.h", "conv_tower_bwd_many.h")
 TRAFFIC = {
-    ("rmsprop", 32, "bf16"): (66.20e6, _RMS_SRC, "82b317f926f0d5b2a0d8c862b73dbdd27a33bce2", "profiles/hbm_traffic_b32.txt"),
-    ("wgrad_all", 32, "bf16"): (22.07e6, _WG_SRC, "bbfce0afc3be1586d967ec049d52523d946994d8", "profiles/hbm_traffic_b32.txt"),
-    ("conv_tower", 32, "bf16"): (10.24e6, _TOWER_SRC, "3970e14bdadcbf6f3de37a34778e44cabca75de4", "profiles/hbm_traffic_b32.txt"),
-    ("conv_tower_bwd", 32, "bf16"): (4.77e6, _TOWER_BWD_SRC, "504b5c772d8dbc081015c5fd66607badce5d5f45", "profiles/hbm_traffic_b32.txt"),
-    ("rmsprop", 256, "bf16"): (71.38e6, _RMS_SRC, "82b317f926f0d5b2a0d8c862b73dbdd27a33bce2", "profiles/hbm_traffic_b256.txt"),
-    ("wgrad_all", 256, "bf16"): (58.68e6, _WG_SRC, "bbfce0afc3be1586d967ec049d52523d946994d8", "profiles/hbm_traffic_b256.txt"),
-    ("conv_tower", 256, "bf16"): (24.35e6, _TOWER_SRC, "3970e14bdadcbf6f3de37a34778e44cabca75de4", "profiles/hbm_traffic_b256.txt"),
-    ("conv_tower_bwd", 256, "bf16"): (23.43e6, _TOWER_BWD_SRC, "504b5c772d8dbc081015c5fd66607badce5d5f45", "profiles/hbm_traffic_b256.txt"),
+    ("rmsprop", 32, "bf16"): (66.20e6, _RMS_SRC, "17139192e59f7d69de571bc16f307bb6032cf26a", "profiles/hbm_traffic_b32.txt"),
+    ("wgrad_all", 32, "bf16"): (22.07e6, _WG_SRC, "708f56153d55ff13051e2d36e48f0d49a6714fe2", "profiles/hbm_traffic_b32.txt"),
+    ("conv_tower", 32, "bf16"): (10.24e6, _TOWER_SRC, "ccc84e80d518ab81091b29dec456fc5c534c8581", "profiles/hbm_traffic_b32.txt"),
+    ("conv_tower_bwd", 32, "bf16"): (4.77e6, _TOWER_BWD_SRC, "d4cd9b2f6cf01c1fd11b7ea208345ccdc2dce88d", "profiles/hbm_traffic_b32.txt"),
+    ("rmsprop", 256, "bf16"): (71.38e6, _RMS_SRC, "17139192e59f7d69de571bc16f307bb6032cf26a", "profiles/hbm_traffic_b256.txt"),
+    ("wgrad_all", 256, "bf16"): (58.67e6, _WG_SRC, "708f56153d55ff13051e2d36e48f0d49a6714fe2", "profiles/hbm_traffic_b256.txt"),
+    ("conv_tower", 256, "bf16"): (24.35e6, _TOWER_SRC, "ccc84e80d518ab81091b29dec456fc5c534c8581", "profiles/hbm_traffic_b256.txt"),
+    ("conv_tower_bwd", 256, "bf16"): (23.43e6, _TOWER_BWD_SRC, "d4cd9b2f6cf01c1fd11b7ea208345ccdc2dce88d", "profiles/hbm_traffic_b256.txt"),
 }
 
 
