@@ -103,13 +103,11 @@ def test_pitches_and_alignments(kernel):
             p.check()
 
 
-@pytest.mark.parametrize("kernel", list(SIZES))
+@pytest.mark.parametrize("kernel", [k for k in SIZES if k != "q8_stream_kernel 16 4 4"])   # (takes a short k only)
 def test_longest_sums_stay_exact(kernel):
     """K at its limit with all levels -128: the sum is 2^31 - 2^14, the largest there is."""
     K = P.Q8_LINEAR_MAX_K
     M, N, _ = SIZES[kernel]
-    if kernel == "q8_stream_kernel 16 4 4":
-        pytest.skip("takes short k only")
     ld = pitches(kernel, K)
     x, w = (torch.full((r, ld), -128, dtype=torch.int8, device="cuda") for r in (M, N))
     sx, sw = torch.ones(M, device="cuda"), torch.ones(N, device="cuda")
